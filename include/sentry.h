@@ -65,7 +65,8 @@ typedef enum {
 /* SENTRY_F16 (IEEE half; the FP16 post-training-quantisation point of Sec. 5): taken by every entry point.  The
  * FFN pair and the Sparse-MoE block run on tcgen05 with fp16 operands, attention on the warp-MMA kernels with fp16
  * operands (the tcgen05 attention kernel is bf16 only), the projections on tcgen05 with fp16 operands. */
-typedef enum { SENTRY_F32 = 0, SENTRY_BF16 = 1, SENTRY_F16 = 2, SENTRY_FP8_E4M3 = 3 /* FFN only, see sentry_ffn_fwd_fp8 */ } sentry_dtype;
+typedef enum { SENTRY_F32 = 0, SENTRY_BF16 = 1, SENTRY_F16 = 2, SENTRY_FP8_E4M3 = 3 /* FFN and cache codes only, see sentry_ffn_fwd_fp8, sentry_kv_cache */,
+               SENTRY_I8 = 4 /* cache codes only */ } sentry_dtype;
 
 /* Create / destroy a context bound to CUDA device `device`.  Creation
  * allocates one small device status word; nothing else. */
@@ -474,6 +475,121 @@ SENTRY_API int sentry_ffn_fwd(sentry_ctx* ctx, const sentry_ffn_desc* desc, cons
                    const void* W1, const void* W2, const int32_t* kept_channels,
                    const int32_t* list_of_sample, const int32_t* token_modality_ids,
                    const uint32_t* masks, void* Y, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit integer products (Sec. 5, the post-training-quantisation axis; the integer point beside FP8): a linear layer
+ * whose activations are quantised per token when they arrive and whose weights were quantised per output channel once.
+ *
+ * sentry_quantize_rows_i8: for every row m of X [M,K] (dtype F32, BF16 or F16)
+ *   scales[m] = max_k |x_mk| * fl(1/127)       (in fp32; at least 2^-126 where the row has a value other than 0; else 0)
+ *   codes[m,k] = x_mk / scales[m], the exact quotient to the nearest integer, ties to even, in [-127,127]; 0 where the scale is 0
+ * A row that holds a NaN or an infinity has a NaN scale and zero codes, so that what is made of it is NaN.
+ * The same call quantises weights stored [N,K]: a row is then an output channel.
+ *   codes out [M,K] i8; scales out [M] fp32.  K % 16 == 0, K <= 65536; M >= 0.
+ *
+ * sentry_linear_i8: Y[m,n] = x_scales[m] * w_scales[n] * (sum_k codes[m,k] * W[n,k]) + bias[n]
+ *   codes [M,K] i8; W [N,K] i8 (an output channel is a row); x_scales [M], w_scales [N], bias [N] or NULL: fp32
+ *   Y out [M,N] in desc->dtype
+ * The sum is exact (32-bit integers; every code in [-128,127]), scaled in fp32 and rounded once.  K % 16 == 0, K <= 65536,
+ * M, N >= 0 of any size.  Neither call uses the workspace.  codes, W, X and Y: 16-byte aligned.
+ */
+typedef struct sentry_linear_desc {
+    int M, K, N;
+    int dtype; /* sentry_dtype of Y */
+} sentry_linear_desc;
+SENTRY_API int sentry_quantize_rows_i8(sentry_ctx* ctx, int M, int K, int dtype, const void* X, int8_t* codes, float* scales, void* stream);
+SENTRY_API int sentry_linear_i8(sentry_ctx* ctx, const sentry_linear_desc* desc, const int8_t* codes, const float* x_scales, const int8_t* W,
+                     const float* w_scales, const float* bias, void* Y, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Cross attention: the rows of a decoder (or of a fusion head's queries) on the encoder's states of the same sample, of
+ * another length.  Dense: every row sees every present key.  Per sample b, kept head h = kept_heads[b,j], KV group
+ * g = floor(h / (Hq/Hk)):
+ *   O[b,j,i] = softmax_n(q_i . k_n / sqrt(d)) V,  n over the present keys of sample b
+ * Key n is present iff n < key_lengths[b] (where key_lengths is given; values above Tk mean Tk, negative ones 0) and the
+ * bit key_modality_ids[n] of masks[b] is set (where those are given).  A sample without a present key gets zero rows; no
+ * status bit is raised for it.  What K and V hold at absent keys is not read into any result, be it NaN or infinite.
+ *   Q [B,Hq,Tq,d]; K, V [B,Hk,Tk,d]; O out [B,k_h,Tq,d], contiguous, heads in kept-list order
+ *   kept_heads [B,k_h] i32 or NULL (k_h == Hq, every head).  An entry outside [0,Hq) gives zero rows and BAD_INDEX.
+ *   key_modality_ids [Tk] i32 + masks [B] u32, or both NULL; an id outside [0,32) is absent
+ * Strides in elements, multiples of 8 for the 16-bit types and of 4 for F32 (a token's d values are contiguous; Q, K and V
+ * may be views of one projection's result); all three 0 = contiguous.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
+ * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24.
+ * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (relative 2^-9, 2^-12),
+ * in the form for few rows as a rounded head and a remainder.
+ * Workspace: sentry_cross_workspace_bytes.
+ */
+typedef struct sentry_cross_desc {
+    int B, Tq, Tk;         /* batch, rows per sample, keys per sample */
+    int Hq, Hk, d;
+    int k_h;               /* kept heads per sample */
+    int dtype;             /* sentry_dtype of Q, K, V, O */
+    int64_t q_stride[3], k_stride[3], v_stride[3]; /* batch, head, token */
+} sentry_cross_desc;
+SENTRY_API size_t sentry_cross_workspace_bytes(const sentry_cross_desc* desc);
+SENTRY_API int sentry_cross_attend_fwd(sentry_ctx* ctx, const sentry_cross_desc* desc, const void* Q, const void* K, const void* V,
+                            const int32_t* kept_heads, const int32_t* key_modality_ids, const uint32_t* masks,
+                            const int32_t* key_lengths, void* O, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A cache of keys and values in 8 bits with one scale per page (a block of `page` tokens) and KV head, and attention over it.
+ * Only present tokens are stored, so nothing of an absent modality is read again.
+ *
+ * The pool belongs to the caller:
+ *   k, v                [n_pages, Hk, page, d] codes: e4m3 (SENTRY_FP8_E4M3) or i8 (SENTRY_I8); value = code * scale
+ *   k_scales, v_scales  [n_pages, Hk] fp32
+ *   page_table          [B, max_pages] i32: the pages of every sample in order; token t of a sample lies in slot t % page of
+ *                       page page_table[b, t / page].  Entries behind a sample's tokens are not read.  An entry outside
+ *                       [0,n_pages) that is needed raises BAD_INDEX: nothing is stored there, its tokens are not seen.
+ * Pages may be shared by samples that only read them (several decoders over one encoder's states).  A page that is
+ * appended to belongs to one place of one sample alone.
+ */
+typedef struct sentry_kv_cache {
+    int Hk, d, page, n_pages, max_pages; /* d in {16,32,64,128}, page in {16,32,64,128} */
+    int format;                          /* SENTRY_FP8_E4M3 or SENTRY_I8 */
+    void *k, *v;                         /* 16-byte aligned */
+    float *k_scales, *v_scales;
+    const int32_t* page_table;
+} sentry_kv_cache;
+
+/* Stores the present tokens of K, V behind the first lengths[b] tokens of every sample, in their order.
+ *   K, V [B,Hk,T,d] (dtype F32, BF16, F16; strides as for cross attention)
+ *   token t is present iff t < token_lengths[b] (or NULL) and the bit token_modality_ids[t] of masks[b] is set (or both NULL)
+ *   lengths [B] i32 (read); new_lengths [B] i32 out: lengths[b] + stored tokens.  They must not overlap.
+ * The scale of a page and head, for the tokens that this call puts there and with a = the largest |value| among them:
+ *   i8    a * fl(1/127) in fp32, at least 2^-126; e4m3: the smallest power of two, at least 2^-126, with a / scale <= 448; 0 for a = 0
+ * and never less than what a partly filled page has already: where it grows, the page's older codes are rounded again under
+ * the new scale.  A page that starts with this call takes nothing from what it held.  Codes are the nearest to the exact
+ * quotient value / scale, ties to even.  A page and head that receives a NaN or an infinity has a NaN scale and zero codes, and
+ * keeps the NaN for as long as the page holds tokens of before.
+ * Tokens beyond max_pages * page are not stored and raise BAD_INDEX; new_lengths stays within the capacity.  A length outside
+ * [0, max_pages * page] stores nothing, raises BAD_INDEX and is clamped.
+ * Slots behind the new length, other pages and their scales keep what they held.  No workspace.
+ */
+typedef struct sentry_append_desc {
+    int B, T, dtype;
+    int64_t k_stride[3], v_stride[3];
+} sentry_append_desc;
+SENTRY_API int sentry_cache_append(sentry_ctx* ctx, const sentry_kv_cache* cache, const sentry_append_desc* desc, const void* K, const void* V,
+                        const int32_t* token_modality_ids, const uint32_t* masks, const int32_t* token_lengths,
+                        const int32_t* lengths, int32_t* new_lengths, void* stream);
+
+/* Attention of Tq rows per sample over the first lengths[b] tokens of the cache:
+ *   O[b,j,i] = softmax_n(q_i . k_n / sqrt(d)) V,  n < lengths[b], and with causal != 0 also n <= lengths[b] - Tq + i (the
+ *   rows are the sample's last Tq tokens, which have been appended before)
+ *   Q [B,Hq,Tq,d] (strided as above), O out [B,k_h,Tq,d]; dtype F32, BF16 or F16; kept_heads as for cross attention
+ * A row without a visible key is zero.  Lengths outside [0, max_pages * page] are clamped.
+ * 16-bit Q meets the codes as fp16, each row scaled by a power of two so that its largest value lies in [1,2) (what the row has
+ * below 2^-14 of it loses digits); the softmax weights are fp16 too, as a head and a remainder where O is fp16; all sums are fp32.
+ * e4m3 codes 0x7f and 0xff (NaN; sentry_cache_append writes none) give NaN.  Workspace: sentry_cache_workspace_bytes.
+ */
+typedef struct sentry_cache_attend_desc {
+    int B, Tq, Hq, k_h, dtype, causal;
+    int64_t q_stride[3];
+} sentry_cache_attend_desc;
+SENTRY_API size_t sentry_cache_workspace_bytes(const sentry_kv_cache* cache, const sentry_cache_attend_desc* desc);
+SENTRY_API int sentry_cache_attend_fwd(sentry_ctx* ctx, const sentry_kv_cache* cache, const sentry_cache_attend_desc* desc, const void* Q,
+                            const int32_t* kept_heads, const int32_t* lengths, void* O, void* stream);
 
 /* Self-test of the bounded device waits.  Every wait inside the kernels (on a
  * TMA copy, a tensor-core commit, another warp) gives up after about a second,

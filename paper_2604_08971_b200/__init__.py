@@ -20,7 +20,7 @@ from . import build as _build
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsentry.so")
 
-SENTRY_F32, SENTRY_BF16, SENTRY_F16, SENTRY_FP8_E4M3 = 0, 1, 2, 3
+SENTRY_F32, SENTRY_BF16, SENTRY_F16, SENTRY_FP8_E4M3, SENTRY_I8 = 0, 1, 2, 3, 4
 STATUS_BIT_TIMEOUT, STATUS_BIT_EMPTY_MASK, STATUS_BIT_BAD_INDEX = 1, 2, 4
 OPT_ATTEND_KERNEL = 1
 ATTEND_AUTO, ATTEND_WARP_MMA, ATTEND_TCGEN05 = 0, 1, 2
@@ -34,7 +34,9 @@ EXPORTS = ["sentry_create", "sentry_destroy", "sentry_get_last_status", "sentry_
            "sentry_kernel_name", "sentry_gate_select_static", "sentry_selftest_wait_expiry", "sentry_set_option",
            "sentry_ffn_packed_bytes", "sentry_ffn_prepack", "sentry_ffn_prepack_fp8", "sentry_ffn_fwd_fp8", "sentry_ffn_fwd_packed",
            "sentry_gate_eval", "sentry_gate_layer_counts", "sentry_project_qkv", "sentry_project_out",
-           "sentry_gate_select_multi", "sentry_sample_table_arrange", "sentry_gate_attend_fwd", "sentry_moe_workspace_bytes", "sentry_moe_packed_bytes", "sentry_moe_prepack", "sentry_moe_ffn_fwd"]
+           "sentry_gate_select_multi", "sentry_sample_table_arrange", "sentry_gate_attend_fwd", "sentry_moe_workspace_bytes", "sentry_moe_packed_bytes", "sentry_moe_prepack", "sentry_moe_ffn_fwd",
+           "sentry_quantize_rows_i8", "sentry_linear_i8", "sentry_cross_workspace_bytes", "sentry_cross_attend_fwd",
+           "sentry_cache_append", "sentry_cache_workspace_bytes", "sentry_cache_attend_fwd"]
 
 
 class AttendDesc(ctypes.Structure):
@@ -61,6 +63,28 @@ GATE_MAX_SETS = 4
 
 class MoeDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("N", "D", "F", "E", "top_k", "k_c", "dtype")]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("M", "K", "N", "dtype")]
+
+
+class CrossDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "Tq", "Tk", "Hq", "Hk", "d", "k_h", "dtype")]
+                + [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride")])
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("Hk", "d", "page", "n_pages", "max_pages", "format")]
+                + [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales", "page_table")])
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "T", "dtype")] + [(n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride")])
+
+
+class CacheAttendDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "Tq", "Hq", "k_h", "dtype", "causal")] + [("q_stride", ctypes.c_int64 * 3)])
 
 
 class SentryError(RuntimeError):
@@ -123,6 +147,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sentry_moe_packed_bytes.restype = ctypes.c_size_t
     lib.sentry_moe_prepack.argtypes = [vp, ctypes.POINTER(MoeDesc), vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sentry_moe_ffn_fwd.argtypes = [vp, ctypes.POINTER(MoeDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sentry_quantize_rows_i8.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp]
+    lib.sentry_linear_i8.argtypes = [vp, ctypes.POINTER(LinearDesc), vp, vp, vp, vp, vp, vp, vp]
+    lib.sentry_cross_workspace_bytes.argtypes = [ctypes.POINTER(CrossDesc)]
+    lib.sentry_cross_workspace_bytes.restype = ctypes.c_size_t
+    lib.sentry_cross_attend_fwd.argtypes = [vp, ctypes.POINTER(CrossDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sentry_cache_append.argtypes = [vp, ctypes.POINTER(KvCache), ctypes.POINTER(AppendDesc), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sentry_cache_workspace_bytes.argtypes = [ctypes.POINTER(KvCache), ctypes.POINTER(CacheAttendDesc)]
+    lib.sentry_cache_workspace_bytes.restype = ctypes.c_size_t
+    lib.sentry_cache_attend_fwd.argtypes = [vp, ctypes.POINTER(KvCache), ctypes.POINTER(CacheAttendDesc), vp, vp, vp, vp, vp]
     lib.sentry_profile_enable.argtypes = [vp, ci]
     lib.sentry_profile_slots.argtypes = []
     lib.sentry_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_float),
@@ -131,7 +164,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sentry_kernel_name.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("sentry_status_string", "sentry_workspace_bytes", "sentry_kernel_name",
-                        "sentry_ffn_packed_bytes", "sentry_moe_workspace_bytes", "sentry_moe_packed_bytes"):
+                        "sentry_ffn_packed_bytes", "sentry_moe_workspace_bytes", "sentry_moe_packed_bytes",
+                        "sentry_cross_workspace_bytes", "sentry_cache_workspace_bytes"):
             getattr(lib, name).restype = ci
     if path is None:
         _lib = lib
@@ -218,6 +252,8 @@ class Sentry:
         self._handle = h.value
         self._ws = None
         self._ws_bytes = 0
+        self._captured = False      # a call was captured into a graph, which goes on using the workspace of that time
+        self._kept_ws = []
         self.ensure_workspace(1 << 20)
 
     def close(self):
@@ -234,6 +270,9 @@ class Sentry:
     # -- workspace ---------------------------------------------------------
     def ensure_workspace(self, nbytes: int):
         if self._ws is None or self._ws.numel() < nbytes:
+            if self._captured:
+                self._kept_ws.append(self._ws)
+                self._captured = torch.cuda.is_current_stream_capturing()
             self._ws = torch.empty((int(nbytes),), dtype=torch.uint8, device="cuda:%d" % self.device)
             rc = self.lib.sentry_set_workspace(self.h, self._ws.data_ptr(), self._ws.numel())
             if rc != 0:
@@ -480,3 +519,36 @@ class Sentry:
         _binding.moe_ffn_fwd(self, self._handle, self._ws_bytes, X, expert_ids, expert_weights, W1, W2, kept_channels, packed,
                              F, E, k_c, Y)
         return Y
+
+    # -- serving in 8 bits, cross attention -----------------------------------
+    def quantize_rows_i8(self, X, codes=None, scales=None):
+        """sentry_quantize_rows_i8.  X [..., K] -> codes int8 [..., K], scales fp32 [...] (one per row)."""
+        if codes is None:
+            codes = torch.empty(X.shape, dtype=torch.int8, device=X.device)
+        if scales is None:
+            scales = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
+        _binding.quantize_rows_i8(self, self._handle, self._ws_bytes, X, codes, scales)
+        return codes, scales
+
+    def linear_i8(self, codes, x_scales, W, w_scales, bias=None, dtype=torch.bfloat16, Y=None):
+        """sentry_linear_i8.  codes int8 [..., K], x_scales [...]; W int8 [N, K], w_scales, bias fp32 [N].  Returns Y [..., N]
+        in `dtype` (or in Y's)."""
+        return _binding.linear_i8(self, self._handle, self._ws_bytes, codes, x_scales, W, w_scales, bias, dtype, Y)
+
+    def cross_attend_fwd(self, Q, K, V, kept_heads=None, key_modality_ids=None, masks=None, key_lengths=None, O=None):
+        """sentry_cross_attend_fwd.  Q [B,Hq,Tq,d], K, V [B,Hk,Tk,d] (views with a contiguous last dimension are taken as they lie).
+        Returns O [B,k_h,Tq,d]."""
+        return _binding.cross_attend_fwd(self, self._handle, self._ws_bytes, Q, K, V, kept_heads, key_modality_ids, masks, key_lengths, O)
+
+    def cache_append(self, K, V, k_codes, v_codes, k_scales, v_scales, page_table, lengths, token_modality_ids=None, masks=None,
+                     token_lengths=None, new_lengths=None):
+        """sentry_cache_append.  K, V [B,Hk,T,d] behind the first lengths [B] tokens of the samples' pages, in place.  Codes
+        [n_pages,Hk,page,d]: int8, or uint8 / float8_e4m3fn for e4m3; scales fp32 [n_pages,Hk]; page_table int32 [B,max_pages].
+        Returns the new lengths [B]."""
+        return _binding.cache_append(self, self._handle, self._ws_bytes, K, V, k_codes, v_codes, k_scales, v_scales, page_table, lengths,
+                                     token_modality_ids, masks, token_lengths, new_lengths)
+
+    def cache_attend_fwd(self, Q, k_codes, v_codes, k_scales, v_scales, page_table, lengths, kept_heads=None, causal=False, O=None):
+        """sentry_cache_attend_fwd.  Q [B,Hq,Tq,d]; the cache as in cache_append.  Returns O [B,k_h,Tq,d]."""
+        return _binding.cache_attend_fwd(self, self._handle, self._ws_bytes, Q, k_codes, v_codes, k_scales, v_scales, page_table, lengths,
+                                         kept_heads, int(causal), O)

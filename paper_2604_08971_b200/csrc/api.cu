@@ -120,7 +120,8 @@ int sentry_profile_slots(void) { return KS_COUNT; }
 const char* sentry_kernel_name(int slot) {
     static const char* names[KS_COUNT] = {"gate_rows", "gate_expand", "attend_score", "attend_select",
                                           "attend_core", "ffn_prepare", "ffn_main", "gate_eval", "project_qkv", "project_out",
-                                          "moe_plan", "moe_combine", "table_arrange"};
+                                          "moe_plan", "moe_combine", "table_arrange", "quantize_rows", "linear_i8", "kv_attend",
+                                          "kv_combine", "kv_plan", "cache_append"};
     return (slot >= 0 && slot < KS_COUNT) ? names[slot] : "?";
 }
 

@@ -11,10 +11,13 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <string>
 #include <type_traits>
 
@@ -107,6 +110,10 @@ struct Call {
         ws = integer(args[2]);
     }
     void workspace(size_t bytes) {
+        // (a captured graph goes on using the workspace it was captured with: the owner keeps that one)
+        if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None &&
+            PyObject_SetAttrString(owner, "_captured", Py_True) != 0)
+            throw Raised{};
         if ((long long)bytes <= ws) return;
         PyObject* r = PyObject_CallMethod(owner, "ensure_workspace", "n", (Py_ssize_t)bytes);
         if (r == nullptr) throw Raised{};
@@ -379,6 +386,201 @@ METHOD(moe_ffn_fwd) {   // X, expert_ids, expert_weights, W1, W2, kept_channels,
     });
 }
 
+// --------------------------------------------------------------------------------------- serving
+// Tensors of one call: all on the context's device, whose current stream takes the call.
+struct Serving {
+    Call& c;
+    long long device;
+    const char* what;
+    Serving(Call& call, const char* name) : c(call), what(name) {
+        PyObject* o = PyObject_GetAttrString(c.owner, "device");
+        if (o == nullptr) throw Raised{};
+        device = PyLong_AsLongLong(o);
+        Py_DECREF(o);
+        if (device == -1 && PyErr_Occurred()) throw Raised{};
+    }
+    [[noreturn]] void refuse(const char* why) const { raise(PyExc_ValueError, std::string(what) + ": " + why); }
+    const at::Tensor& on_device(const at::Tensor& t) const {
+        if (!t.is_cuda()) raise(PyExc_ValueError, "libsentry takes device tensors (got a " + t.device().str() + " tensor)");
+        if (t.device().index() != device) refuse("a tensor is on another device than the context");
+        return t;
+    }
+    // A contiguous tensor of this type and shape (-1: any extent); None where that is allowed.
+    template <typename T = void>
+    T* dense(const at::Tensor& t, at::ScalarType type, std::initializer_list<int64_t> shape, const char* name) const {
+        on_device(t);
+        bool ok = t.scalar_type() == type && t.dim() == (int64_t)shape.size();
+        size_t i = 0;
+        for (int64_t n : shape) {
+            if (!ok) break;
+            ok = n < 0 || t.size(i) == n;
+            ++i;
+        }
+        if (!ok) refuse((std::string("unexpected type or shape of ") + name).c_str());
+        if (!t.is_contiguous()) raise(PyExc_ValueError, "libsentry takes contiguous tensors");
+        return (T*)t.data_ptr();
+    }
+    template <typename T = void>
+    T* dense(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> shape, const char* name) const {
+        return o == Py_None ? nullptr : dense<T>(tensor(o), type, shape, name);
+    }
+    // bit patterns: int32 or uint32
+    const uint32_t* masks(PyObject* o, int64_t B) const {
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = tensor(o);
+        return dense<uint32_t>(t, t.scalar_type() == at::kUInt32 ? at::kUInt32 : at::kInt, {B}, "masks");
+    }
+    // A [B,H,T,d] view whose last dimension is contiguous: its strides, or zeros for a contiguous one.
+    void* view(const at::Tensor& t, int64_t stride[3]) const {
+        on_device(t);
+        stride[0] = stride[1] = stride[2] = 0;
+        if (t.is_contiguous()) return t.data_ptr();
+        if (t.size(3) > 1 && t.stride(3) != 1) refuse("the last dimension has to be contiguous");
+        for (int i = 0; i < 3; ++i) stride[i] = t.size(i) > 1 ? t.stride(i) : t.size(1) * t.size(2) * t.size(3);
+        if (stride[0] == 0 && stride[1] == 0 && stride[2] == 0) refuse("a tensor that is expanded along every dimension");
+        return t.data_ptr();
+    }
+    void* stream() const { return (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
+};
+int fits(int64_t n) {
+    if (n > 0x7fffffffLL) raise(PyExc_ValueError, "a dimension of 2^31 or more");
+    return (int)n;
+}
+at::ScalarType scalar_type(PyObject* o) {
+    if (!THPDtype_Check(o)) raise(PyExc_TypeError, "expected a dtype");
+    return reinterpret_cast<THPDtype*>(o)->scalar_type;
+}
+int code_format(const at::Tensor& t) {
+    switch (t.scalar_type()) {
+        case at::kChar: return SENTRY_I8;
+        case at::kByte: case at::kFloat8_e4m3fn: return SENTRY_FP8_E4M3;
+        default: raise(PyExc_ValueError, std::string("cache codes are int8, or uint8 / float8_e4m3fn for e4m3: got ") + c10::toString(t.scalar_type()));
+    }
+}
+
+METHOD(quantize_rows_i8) {   // X, codes, scales
+    return guarded(args, n, 3, [](Call& c) {
+        const Serving v(c, "quantize_rows_i8");
+        const at::Tensor &X = v.on_device(tensor(c.a[0])), &codes = v.on_device(tensor(c.a[1])), &scales = v.on_device(tensor(c.a[2]));
+        if (X.dim() < 1) v.refuse("a tensor of one dimension at least");
+        const int K = fits(X.size(-1)), M = K ? fits(X.numel() / K) : 0;
+        if (codes.sizes() != X.sizes() || codes.scalar_type() != at::kChar || scales.scalar_type() != at::kFloat || scales.numel() != M)
+            v.refuse("int8 codes of X's shape and an fp32 scale per row");
+        const int type = dtype_code(X);
+        const void* x = ptr(X);
+        int8_t* cp = ptr<int8_t>(codes);
+        float* sp = ptr<float>(scales);
+        void* st = v.stream();
+        invoke("sentry_quantize_rows_i8", [&] { return sentry_quantize_rows_i8(c.ctx, M, K, type, x, cp, sp, st); });
+    });
+}
+METHOD(linear_i8) {   // codes, x_scales, W, w_scales, bias, dtype, Y
+    return guarded(args, n, 7, [](Call& c) -> at::Tensor {
+        const Serving v(c, "linear_i8");
+        const at::Tensor &X = v.on_device(tensor(c.a[0])), &W = tensor(c.a[2], 2), &xs = v.on_device(tensor(c.a[1]));
+        if (X.dim() < 1 || X.scalar_type() != at::kChar) v.refuse("int8 codes");
+        sentry_linear_desc d;
+        d.K = fits(X.size(-1)); d.M = d.K ? fits(X.numel() / d.K) : 0; d.N = fits(W.size(0));
+        if (xs.scalar_type() != at::kFloat || xs.numel() != d.M) v.refuse("an fp32 scale per row");
+        const int8_t* x = ptr<int8_t>(X);
+        const int8_t* w = v.dense<int8_t>(W, at::kChar, {d.N, d.K}, "W");
+        const float *sx = ptr<float>(xs), *sw = v.dense<float>(c.a[3], at::kFloat, {d.N}, "w_scales"), *bias = v.dense<float>(c.a[4], at::kFloat, {d.N}, "bias");
+        at::Tensor Y;
+        if (c.a[6] != Py_None) {
+            Y = v.on_device(tensor(c.a[6]));
+            if (Y.numel() != (int64_t)d.M * d.N || Y.size(-1) != d.N) v.refuse("an output of another shape");
+        } else {
+            auto shape = X.sizes().vec();
+            shape.back() = d.N;
+            Y = at::empty(shape, X.options().dtype(scalar_type(c.a[5])));
+        }
+        d.dtype = dtype_code(Y);
+        void *y = ptr(Y), *st = v.stream();
+        invoke("sentry_linear_i8", [&] { return sentry_linear_i8(c.ctx, &d, x, sx, w, sw, bias, y, st); });
+        return Y;
+    });
+}
+METHOD(cross_attend_fwd) {   // Q, K, V, kept_heads, ids, masks, key_lengths, O
+    return guarded(args, n, 8, [](Call& c) -> at::Tensor {
+        const Serving v(c, "cross_attend_fwd");
+        const at::Tensor &Q = tensor(c.a[0], 4), &K = tensor(c.a[1], 4), &V = tensor(c.a[2], 4);
+        sentry_cross_desc d;
+        d.B = fits(Q.size(0)); d.Hq = fits(Q.size(1)); d.Tq = fits(Q.size(2)); d.d = fits(Q.size(3));
+        d.Hk = fits(K.size(1)); d.Tk = fits(K.size(2)); d.dtype = dtype_code(Q);
+        if (K.sizes() != V.sizes() || K.size(0) != d.B || K.size(3) != d.d || K.scalar_type() != Q.scalar_type() || V.scalar_type() != Q.scalar_type())
+            v.refuse("K and V of one shape, with Q's batch, head dimension and type");
+        d.k_h = c.a[3] == Py_None ? d.Hq : fits(tensor(c.a[3], 2).size(1));
+        void *q = v.view(Q, d.q_stride), *k = v.view(K, d.k_stride), *val = v.view(V, d.v_stride);
+        const int32_t* kept = v.dense<int32_t>(c.a[3], at::kInt, {d.B, d.k_h}, "kept_heads");
+        const int32_t* ids = v.dense<int32_t>(c.a[4], at::kInt, {d.Tk}, "key_modality_ids");
+        const uint32_t* masks = v.masks(c.a[5], d.B);
+        const int32_t* lengths = v.dense<int32_t>(c.a[6], at::kInt, {d.B}, "key_lengths");
+        at::Tensor O = output(c.a[7], {d.B, d.k_h, d.Tq, d.d}, Q.scalar_type(), Q);
+        void* o = v.dense(O, Q.scalar_type(), {d.B, d.k_h, d.Tq, d.d}, "O");
+        c.workspace(sentry_cross_workspace_bytes(&d));
+        void* st = v.stream();
+        invoke("sentry_cross_attend_fwd", [&] { return sentry_cross_attend_fwd(c.ctx, &d, q, k, val, kept, ids, masks, lengths, o, st); });
+        return O;
+    });
+}
+sentry_kv_cache cache_of(const Serving& v, PyObject* k, PyObject* vals, PyObject* ks, PyObject* vs, PyObject* table, int64_t B) {
+    const at::Tensor &K = tensor(k, 4), &V = tensor(vals, 4);
+    sentry_kv_cache c;
+    c.n_pages = fits(K.size(0)); c.Hk = fits(K.size(1)); c.page = fits(K.size(2)); c.d = fits(K.size(3));
+    c.format = code_format(K);
+    if (code_format(V) != c.format) v.refuse("keys and values of one format");
+    c.k = v.dense(K, K.scalar_type(), {-1, -1, -1, -1}, "the key codes");
+    c.v = v.dense(V, V.scalar_type(), {c.n_pages, c.Hk, c.page, c.d}, "the value codes");
+    c.k_scales = v.dense<float>(tensor(ks), at::kFloat, {c.n_pages, c.Hk}, "k_scales");
+    c.v_scales = v.dense<float>(tensor(vs), at::kFloat, {c.n_pages, c.Hk}, "v_scales");
+    const at::Tensor& t = tensor(table, 2);
+    c.max_pages = fits(t.size(1));
+    c.page_table = v.dense<int32_t>(t, at::kInt, {B, -1}, "page_table");
+    return c;
+}
+METHOD(cache_append) {   // K, V, k, v, k_scales, v_scales, page_table, lengths, ids, masks, token_lengths, new_lengths
+    return guarded(args, n, 12, [](Call& c) -> at::Tensor {
+        const Serving v(c, "cache_append");
+        const at::Tensor &K = tensor(c.a[0], 4), &V = tensor(c.a[1], 4);
+        sentry_append_desc d;
+        d.B = fits(K.size(0)); d.T = fits(K.size(2)); d.dtype = dtype_code(K);
+        const sentry_kv_cache cache = cache_of(v, c.a[2], c.a[3], c.a[4], c.a[5], c.a[6], d.B);
+        if (K.sizes() != V.sizes() || K.scalar_type() != V.scalar_type() || K.size(1) != cache.Hk || K.size(3) != cache.d)
+            v.refuse("K and V of one shape and type, with the cache's heads and head dimension");
+        void *k = v.view(K, d.k_stride), *val = v.view(V, d.v_stride);
+        const at::Tensor& len = tensor(c.a[7]);
+        const int32_t* lengths = v.dense<int32_t>(len, at::kInt, {d.B}, "lengths");
+        const int32_t* ids = v.dense<int32_t>(c.a[8], at::kInt, {d.T}, "token_modality_ids");
+        const uint32_t* masks = v.masks(c.a[9], d.B);
+        const int32_t* most = v.dense<int32_t>(c.a[10], at::kInt, {d.B}, "token_lengths");
+        at::Tensor out = output(c.a[11], {d.B}, at::kInt, len);
+        int32_t* now = v.dense<int32_t>(out, at::kInt, {d.B}, "new_lengths");
+        void* st = v.stream();
+        invoke("sentry_cache_append", [&] { return sentry_cache_append(c.ctx, &cache, &d, k, val, ids, masks, most, lengths, now, st); });
+        return out;
+    });
+}
+METHOD(cache_attend_fwd) {   // Q, k, v, k_scales, v_scales, page_table, lengths, kept_heads, causal, O
+    return guarded(args, n, 10, [](Call& c) -> at::Tensor {
+        const Serving v(c, "cache_attend_fwd");
+        const at::Tensor& Q = tensor(c.a[0], 4);
+        sentry_cache_attend_desc d;
+        d.B = fits(Q.size(0)); d.Hq = fits(Q.size(1)); d.Tq = fits(Q.size(2)); d.dtype = dtype_code(Q); d.causal = small(c.a[8]);
+        d.k_h = c.a[7] == Py_None ? d.Hq : fits(tensor(c.a[7], 2).size(1));
+        const sentry_kv_cache cache = cache_of(v, c.a[1], c.a[2], c.a[3], c.a[4], c.a[5], d.B);
+        if (Q.size(3) != cache.d) v.refuse("Q with the cache's head dimension");
+        void* q = v.view(Q, d.q_stride);
+        const int32_t* lengths = v.dense<int32_t>(c.a[6], at::kInt, {d.B}, "lengths");
+        const int32_t* kept = v.dense<int32_t>(c.a[7], at::kInt, {d.B, d.k_h}, "kept_heads");
+        at::Tensor O = output(c.a[9], {d.B, d.k_h, d.Tq, cache.d}, Q.scalar_type(), Q);
+        void* o = v.dense(O, Q.scalar_type(), {d.B, d.k_h, d.Tq, cache.d}, "O");
+        c.workspace(sentry_cache_workspace_bytes(&cache, &d));
+        void* st = v.stream();
+        invoke("sentry_cache_attend_fwd", [&] { return sentry_cache_attend_fwd(c.ctx, &cache, &d, q, kept, lengths, o, st); });
+        return O;
+    });
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XSETREF(g_error, cls);
@@ -389,6 +591,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 PyMethodDef g_methods[] = {ENTRY(gate_select), ENTRY(gate_select_multi), ENTRY(gate_eval), ENTRY(gate_layer_counts),
                            ENTRY(gate_attend_fwd), ENTRY(attend_fwd), ENTRY(project_qkv), ENTRY(project_out), ENTRY(ffn_fwd),
                            ENTRY(ffn_fwd_packed), ENTRY(ffn_fwd_fp8), ENTRY(ffn_prepack), ENTRY(moe_ffn_fwd),
+                           ENTRY(quantize_rows_i8), ENTRY(linear_i8), ENTRY(cross_attend_fwd), ENTRY(cache_append), ENTRY(cache_attend_fwd),
                            {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

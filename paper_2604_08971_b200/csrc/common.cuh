@@ -19,7 +19,8 @@ constexpr int kSmCount = 148;
 enum KernelSlot {
     KS_GATE_ROWS = 0, KS_GATE_EXPAND, KS_ATT_SCORE, KS_ATT_SELECT, KS_ATT_CORE,
     KS_FFN_PREPARE, KS_FFN_MAIN, KS_GATE_EVAL, KS_PROJ_QKV, KS_PROJ_OUT,
-    KS_MOE_PLAN, KS_MOE_COMBINE, KS_TABLE_ARRANGE, KS_COUNT
+    KS_MOE_PLAN, KS_MOE_COMBINE, KS_TABLE_ARRANGE,
+    KS_QUANTIZE, KS_LINEAR, KS_KV_ATTEND, KS_KV_COMBINE, KS_KV_PLAN, KS_CACHE_APPEND, KS_COUNT
 };
 
 struct ProfRec { cudaEvent_t start, stop; int slot; };

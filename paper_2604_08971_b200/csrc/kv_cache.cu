@@ -1,0 +1,195 @@
+// Storing keys and values in an 8-bit paged cache: codes with one scale per page (a block of tokens) and KV head.
+//
+// A block takes one page of one sample (all heads): it finds the present tokens that land there, and each of its warps takes K or V of
+// one head at a time: the largest magnitude, the page's scale, the codes.  Bound by the bytes of K and V: a warp has all loads of its
+// rows on the way at once (up to kHold pieces of 16 bytes a lane; longer pages are read twice, the second time from the caches).
+#include <cuda_fp8.h>
+
+#include "serving.cuh"
+
+namespace {
+
+constexpr int kAppThreads = 256;
+constexpr int kHold = 16;
+
+__device__ __forceinline__ float nan_f32() { return __int_as_float(0x7fc00000); }
+
+// The scale under which `top` is coded: see sentry_cache_append.
+template <bool I8>
+__device__ __forceinline__ float page_scale(float top) {
+    if (isnan(top)) return top;
+    if constexpr (I8) return scale_i8(top);
+    if (!(top > 0.0f)) return 0.0f;
+    int e;
+    const float m = frexpf(top, &e);     // top = m 2^e, 1/2 <= m < 1; 448 = 7/8 2^9
+    return ldexpf(1.0f, max(e - (m > 0.875f ? 8 : 9), -126));
+}
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+// The e4m3 code nearest to q, where a rounding to fp32 on the way could decide a tie.
+__device__ __noinline__ uint32_t e4m3_of(double q) {
+    int e;
+    frexp(q, &e);
+    const double step = ldexp(1.0, max(e, -5) - 4);
+    return (uint32_t)__nv_cvt_float_to_fp8((float)(rint(q / step) * step), __NV_SATFINITE, __NV_E4M3);
+}
+// Four values under scale s (0 or not a number: zero codes).  This library's e4m3 scales are powers of two, so that x / s = x * inv is
+// exact but for results below e4m3's smallest step, which round to 0 or to it either way; a scale of somebody else's need not be one.
+template <bool I8>
+__device__ __forceinline__ uint32_t four_codes(const float* x, float s, float inv) {
+    if (!(s >= 1.17549435e-38f)) return 0u;
+    if constexpr (I8) {
+        return pack_i8x4(round_quotient_i8(x[0], s, inv), round_quotient_i8(x[1], s, inv), round_quotient_i8(x[2], s, inv), round_quotient_i8(x[3], s, inv));
+    } else {
+        if (__float_as_uint(s) & 0x7fffffu) {
+            uint32_t w = 0;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) w |= e4m3_of((double)x[i] / (double)s) << (8 * i);
+            return w;
+        }
+        return e4m3x2(x[0] * inv, x[1] * inv) | (e4m3x2(x[2] * inv, x[3] * inv) << 16);
+    }
+}
+// A stored code under a larger scale: code * old / now to the nearest code.  (Doubles hold the product exactly, and the quotient to
+// more places than a tie can differ by; rare, so its cost does not matter.)
+template <bool I8>
+__device__ uint8_t again(uint8_t c, float old, float now) {
+    if (!(now > 0.0f)) return 0;
+    if constexpr (I8) {
+        const double q = rint((double)(int8_t)c * (double)old / (double)now);
+        return (uint8_t)(int8_t)(int)fmin(fmax(q, -127.0), 127.0);
+    } else {
+        const __half_raw h = __nv_cvt_fp8_to_halfraw(c, __NV_E4M3);
+        return (uint8_t)e4m3_of((double)__half2float(__half(h)) * (double)old / (double)now);
+    }
+}
+
+template <typename T, bool I8>
+__global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const AppendArgs a, int page_blocks) {
+    constexpr int N = Vec16<T>::N;
+    __shared__ int s_token[128];
+    __shared__ int s_count[kAppThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int b = blockIdx.x / page_blocks, pb = blockIdx.x % page_blocks;
+    const int page = a.c.page, T_ = a.d.T, Hk = a.c.Hk, d = a.c.d;
+    grid_dependents_start_if_small();
+    grid_dependency_wait();
+    const int cap = a.c.max_pages * page;
+    const int given = a.lengths[b];
+    const bool sane = given >= 0 && given <= cap;
+    const int len = min(max(given, 0), cap);
+    const int most = a.token_lengths ? min(max(a.token_lengths[b], 0), T_) : T_;
+    // this block's page: slots [lo, hi) of page `at`, which the present tokens of ranks [lo - slot0, ...) take
+    const int at = len / page + pb;
+    const int start = max(at * page, len);                 // position of its first new token
+    int total = most;                                      // present tokens of the sample
+    if (a.ids != nullptr) {
+        const uint32_t mask = a.masks[b];
+        const int per = (most + kAppThreads - 1) / kAppThreads;
+        const int t0 = min((int)threadIdx.x * per, most), t1 = min(t0 + per, most);
+        int mine = 0;
+        for (int t = t0; t < t1; ++t) {
+            const int m = a.ids[t];
+            mine += m >= 0 && m < 32 && ((mask >> m) & 1u);
+        }
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) s_count[warp] = incl;
+        __syncthreads();
+        int before = incl - mine;
+        total = 0;
+        for (int w = 0; w < kAppThreads / 32; ++w) { if (w < warp) before += s_count[w]; total += s_count[w]; }
+        const int r0 = start - len;
+        for (int t = t0, r = before; t < t1 && r < r0 + page; ++t) {
+            const int m = a.ids[t];
+            if (!(m >= 0 && m < 32 && ((mask >> m) & 1u))) continue;
+            if (r >= r0) s_token[r - r0] = t;
+            ++r;
+        }
+    }
+    const int room = sane ? cap - len : 0, put = min(total, room);
+    if (pb == 0 && threadIdx.x == 0) {
+        a.new_lengths[b] = len + put;
+        if (put < total || !sane) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+    }
+    const int n = min(len + put - start, (at + 1) * page - start);   // new tokens of this page
+    if (n <= 0) return;
+    if (a.ids == nullptr && threadIdx.x < (unsigned)n) s_token[threadIdx.x] = start - len + threadIdx.x;
+    const int id = a.c.page_table[(size_t)b * a.c.max_pages + at];
+    if (id < 0 || id >= a.c.n_pages) {
+        if (threadIdx.x == 0) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+        return;
+    }
+    __syncthreads();
+    const int slot0 = start - at * page;
+    const int per_row = d / N, pieces = n * per_row;       // 16-byte pieces of a row, and of all
+    for (int unit = warp; unit < 2 * Hk; unit += kAppThreads / 32) {
+        const bool is_v = unit >= Hk;
+        const int h = is_v ? unit - Hk : unit;
+        const long long* st = is_v ? a.vs : a.ks;
+        const T* src = (const T*)(is_v ? a.V : a.K) + b * st[0] + h * st[1];
+        uint8_t* codes = (uint8_t*)(is_v ? a.c.v : a.c.k) + ((size_t)id * Hk + h) * page * d;
+        float* scale = (is_v ? a.c.v_scales : a.c.k_scales) + (size_t)id * Hk + h;
+        const float old = slot0 > 0 ? *scale : 0.0f;
+        auto piece = [&](int p) { return *reinterpret_cast<const uint4*>(src + s_token[p / per_row] * st[2] + (p % per_row) * N); };
+        uint4 held[kHold];
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) held[i] = i * 32 + lane < pieces ? piece(i * 32 + lane) : make_uint4(0, 0, 0, 0);
+        float top = 0.0f;
+        bool bad = false;
+        auto look = [&](const uint4& v) {
+            float f[N];
+            Vec16<T>::get(v, f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float m = fabsf(f[j]);
+                bad = bad || !(m <= 3.4028234e38f);
+                top = fmaxf(top, m);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) look(held[i]);
+        for (int p = kHold * 32 + lane; p < pieces; p += 32) look(piece(p));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        bad = __any_sync(0xffffffffu, bad) || isnan(old);
+        const float need = page_scale<I8>(top);
+        const float now = bad ? nan_f32() : fmaxf(need, old);
+        const float inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
+        // older codes of the page under its new scale
+        if (slot0 > 0 && !(now == old))
+            for (int i = lane; i < slot0 * d; i += 32) codes[i] = again<I8>(codes[i], old, now);
+        auto store = [&](const uint4& v, int p) {
+            float f[N];
+            Vec16<T>::get(v, f);
+            uint8_t* dst = codes + (size_t)(slot0 + p / per_row) * d + (p % per_row) * N;
+            if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(four_codes<I8>(f, now, inv), four_codes<I8>(f + 4, now, inv));
+            else *reinterpret_cast<uint32_t*>(dst) = four_codes<I8>(f, now, inv);
+        };
+#pragma unroll
+        for (int i = 0; i < kHold; ++i)
+            if (i * 32 + lane < pieces) store(held[i], i * 32 + lane);
+        for (int p = kHold * 32 + lane; p < pieces; p += 32) store(piece(p), p);
+        if (lane == 0 && !(now == old && slot0 > 0)) *scale = now;
+    }
+}
+
+}  // namespace
+
+int launch_cache_append(sentry_ctx* ctx, const AppendArgs& a, cudaStream_t st) {
+    // pages that T tokens can touch, wherever they start
+    const long long blocks = a.d.T > 0 ? ((long long)a.d.T + a.c.page - 2) / a.c.page + 1 : 1;
+    if (blocks * a.d.B > 0x7fffffffLL) return SENTRY_ERR_UNSUPPORTED;
+    const bool i8 = a.c.format == SENTRY_I8;
+    auto k = a.d.dtype == SENTRY_F32    ? (i8 ? cache_append_kernel<float, true> : cache_append_kernel<float, false>)
+             : a.d.dtype == SENTRY_BF16 ? (i8 ? cache_append_kernel<__nv_bfloat16, true> : cache_append_kernel<__nv_bfloat16, false>)
+                                        : (i8 ? cache_append_kernel<__half, true> : cache_append_kernel<__half, false>);
+    LaunchScope ls(ctx, KS_CACHE_APPEND, st);
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(blocks * a.d.B)), dim3(kAppThreads), 0, st, a, (int)blocks));
+    return SENTRY_OK;
+}

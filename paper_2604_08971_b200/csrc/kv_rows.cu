@@ -1,0 +1,614 @@
+// Serving attention for few rows: a decoder's single tokens and short blocks, over dense 16-bit keys and values or the 8-bit cache.
+//
+// The rows of one KV group (kept heads x Tq) share its keys, so they are packed into tiles of 16 rows, and a block takes a tile and a
+// stretch of the keys.  Each of its four warps walks tiles of 32 keys by itself, with a ring of asynchronous copies of its own, a running
+// maximum and sum of its own (log2 domain), and both products on the warp MMA (16 rows x 8 keys or columns x 16): no barrier until the
+// four partial results meet.  Long axes are split over blocks; kv_combine_kernel joins the parts.
+// What bounds it: the bytes of K and V, read once from memory.  For that the codes go through registers straight into MMA operands:
+// the order of the inner index is free as long as both operands share it, so that a lane's 16 consecutive bytes of a key are its operand
+// for K's product; and for V's, where pairs run along the keys, two keys' words are interleaved byte by byte.  8-bit codes become fp16 exactly; a page's
+// key scale multiplies the scores, its value scale the tile's product before that joins the accumulator (folded into the weights it
+// would cost fp16's range).
+#include "kv_attend.cuh"
+#include "ptx/sm100.cuh"
+
+namespace {
+
+constexpr int kWarps = 4, kKeys = 32, kRowTile = 16;
+constexpr float kLog2e = 1.4426950408889634f;
+
+enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2, KV_I8 = 3 };
+
+template <int KV, int D>
+struct RowsCfg {
+    static constexpr int ESIZE = KV <= KV_F16 ? 2 : 1;
+    static constexpr int ROW = D * ESIZE;                    // bytes of a key
+    static constexpr int CHUNKS = ROW / 16;
+    static constexpr int STAGE = 2 * kKeys * ROW;            // K and V of a tile
+    static constexpr int FIT = 98304 / (kWarps * STAGE);
+    static constexpr int STAGES = FIT < 3 ? 3 : FIT > 6 ? 6 : FIT;
+    static constexpr int RING = kWarps * STAGES * STAGE;
+    static constexpr int MERGE = kWarps * kRowTile * D * 4;
+    static constexpr int SMEM = RING > MERGE ? RING : MERGE;
+};
+
+// Where 16-byte piece `c` of key `r` lies in its row: lanes that read one piece number of eight keys, or several of one, meet different banks.
+template <int CHUNKS>
+__device__ __forceinline__ int swizzled(int r, int c) {
+    const int f = (((r >> 1) & 3) * 2) ^ ((r & 1) * 4);
+    return c ^ (f & (CHUNKS - 1));
+}
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool yes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(yes ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+template <int BYTES>
+__device__ __forceinline__ void lds(uint32_t addr, uint32_t* r) {
+    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+    else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+    else if constexpr (BYTES == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(addr));
+    else {
+        unsigned short v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+        r[0] = v;
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t v;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    return v;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+    if constexpr (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+// two codes in the low 16 bits of w -> fp16 pair
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_hi_to_f16x2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+// bytes (already + 128) -> fp16: 0x6400 | u is 1024 + u, exactly
+__device__ __forceinline__ uint32_t biased_to_f16x2(uint32_t pair) {
+    const uint32_t bias = 0x64806480u;   // 1152
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(bias));
+    return r;
+}
+// four codes of a word, in order, as two fp16 pairs
+template <bool I8>
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& p01, uint32_t& p23) {
+    if constexpr (I8) {
+        const uint32_t u = w ^ 0x80808080u;
+        p01 = biased_to_f16x2(__byte_perm(u, 0x64646464u, 0x4140));
+        p23 = biased_to_f16x2(__byte_perm(u, 0x64646464u, 0x4342));
+    } else {
+        p01 = e4m3x2_to_f16x2(w);
+        p23 = e4m3x2_hi_to_f16x2(w);
+    }
+}
+
+struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
+
+// KV: type of the keys and values; BF16: type of Q and O.  part: [n_splits][B][k_h][Tq][D] sums and ml: [n_splits][B][k_h][Tq] (maximum, total),
+// where the keys are split.
+template <int KV, int D, bool BF16>
+__global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
+    using C = RowsCfg<KV, D>;
+    constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
+    constexpr bool MMA_BF16 = KV == KV_BF16;
+    constexpr bool SPLIT_P = DENSE || !BF16;                 // weights as a head and a remainder
+    constexpr int KSTEPS = D / 16, NTILES = D / 8;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ RowsMeta s_meta[kWarps][C::STAGES];
+    __shared__ short s_head[kServeMaxHeads], s_pos[kServeMaxHeads];
+    __shared__ int s_heads;
+    __shared__ float s_m[kWarps][kRowTile], s_l[kWarps][kRowTile];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, t4 = lane & 3;
+    const int split = blockIdx.x % n_splits, bg = blockIdx.x / n_splits, b = bg / a.Hk, g = bg % a.Hk;
+    grid_dependents_start_if_small();
+    grid_dependency_wait();
+
+    // the kept heads of this group, in the list's order
+    if (warp == 0) {
+        const int per = a.Hq / a.Hk;
+        int n = 0;
+        for (int j0 = 0; j0 < a.k_h; j0 += 32) {
+            const int j = j0 + lane, h = j < a.k_h ? kv_head(a, b, j) : -2;
+            const unsigned mine = __ballot_sync(0xffffffffu, h >= 0 && h / per == g);
+            if ((mine >> lane) & 1u) {
+                const int at = n + __popc(mine & ((1u << lane) - 1u));
+                s_head[at] = (short)h;
+                s_pos[at] = (short)j;
+            }
+            n += __popc(mine);
+            if (h == -1 && g == 0 && split == 0 && blockIdx.y == 0) {   // not a head: zero rows
+                atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                uint32_t* o = (uint32_t*)a.O + ((size_t)b * a.k_h + j) * a.Tq * (D / 2);
+                for (size_t e = 0; e < (size_t)a.Tq * (D / 2); ++e) o[e] = 0u;
+            }
+        }
+        if (lane == 0) s_heads = n;
+    }
+    __syncthreads();
+    const int rows = s_heads * a.Tq;
+    const int len = kv_length(a, b);
+    const uint32_t mask = a.masks ? a.masks[b] : 0u;
+    const int tiles = (len + kKeys - 1) / kKeys;
+    const int per_split = ((tiles + n_splits - 1) / n_splits + kWarps - 1) / kWarps * kWarps;
+    const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles);
+    const uint32_t ring = ptx::smem_u32(smem) + warp * C::STAGES * C::STAGE;
+    RowsMeta* meta = s_meta[warp];
+    const char *kbase, *vbase;
+    if constexpr (DENSE) {
+        kbase = (const char*)a.K + (b * a.ks[0] + g * a.ks[1]) * 2;
+        vbase = (const char*)a.V + (b * a.vs[0] + g * a.vs[1]) * 2;
+    } else {
+        kbase = (const char*)a.K;
+        vbase = (const char*)a.V;
+    }
+
+    for (int row0 = blockIdx.y * kRowTile; row0 < rows; row0 += gridDim.y * kRowTile) {
+        // -------------------------------------------------------------------- this lane's two rows of Q as MMA operands
+        uint32_t qf[KSTEPS][4];
+        float rscale[2];
+        int last[2];                                            // keys that the row sees end here
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = row0 + gq + half * 8;
+            const bool in = r < rows;
+            const int jj = in ? r / a.Tq : 0, i = in ? r % a.Tq : 0;
+            const char* q = (const char*)a.Q + (b * a.qs[0] + (in ? s_head[jj] : 0) * a.qs[1] + i * a.qs[2]) * 2;
+            last[half] = !DENSE && a.causal ? min(len, len - a.Tq + i + 1) : len;
+            uint32_t w[KSTEPS][2];
+            // elements of a chunk that one lane has: 16 bytes of a key, or a quarter of a shorter one
+            constexpr int E = (C::ROW / 4 < 16 ? C::ROW / 4 : 16) / C::ESIZE;
+#pragma unroll
+            for (int s = 0; s < KSTEPS; ++s) {
+                const int e = (s / (E / 4)) * 4 * E + t4 * E + (s % (E / 4)) * 4;
+                const uint2 x = in ? *reinterpret_cast<const uint2*>(q + e * 2) : make_uint2(0, 0);
+                w[s][0] = x.x;
+                w[s][1] = x.y;
+            }
+            float rs = rsqrtf((float)D) * kLog2e;
+            if constexpr (!DENSE && BF16) {
+                // bf16 rows as fp16: scaled by a power of two so that the largest value lies in [1,2)
+                float top = 0.0f;
+#pragma unroll
+                for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float2 f = unpack2<true>(w[s][x]);
+                        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                int e = (int)(__float_as_uint(top) >> 23) - 127;      // (infinities: 128, and the row is not a number in any case)
+                e = min(max(e, -120), 120);
+                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+                rs *= __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+                for (int s = 0; s < KSTEPS; ++s)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float2 f = unpack2<true>(w[s][x]);
+                        w[s][x] = pack2<false>(f.x * down, f.y * down);
+                    }
+            }
+            rscale[half] = rs;
+#pragma unroll
+            for (int s = 0; s < KSTEPS; ++s) { qf[s][half] = w[s][0]; qf[s][2 + half] = w[s][1]; }
+        }
+        float o[NTILES][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[j][x] = 0.0f;
+
+        // -------------------------------------------------------------------- copies
+        // `ahead`: the modality id, or the page, of this lane's key of the tile that is issued next
+        auto look_ahead = [&](int it) -> int {
+            const int n = (t0 + warp + it * kWarps) * kKeys + lane;
+            if (t0 + warp + it * kWarps >= t1 || n >= len) return -1;
+            if constexpr (DENSE) return a.ids ? a.ids[n] : 0;
+            else return a.table[(size_t)b * a.max_pages + n / a.page];
+        };
+        int ahead = look_ahead(0);
+        auto issue = [&](int it) {
+            const int tile = t0 + warp + it * kWarps;
+            if (tile < t1) {
+                const int slot = it % C::STAGES;
+                const uint32_t dst = ring + slot * C::STAGE;
+                const int n0 = tile * kKeys;
+                bool ok = n0 + lane < len;
+                if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
+                else {
+                    const bool good = ahead >= 0 && ahead < a.n_pages;
+                    if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                    ok = ok && good;
+                }
+                const unsigned vis = __ballot_sync(0xffffffffu, ok);
+                if (lane == 0) meta[slot].vis = vis;
+                if (vis != 0) {
+                    if constexpr (!DENSE) {
+                        if ((lane & 15) == 0 && ok) {
+                            const size_t ph = (size_t)ahead * a.Hk + g;
+                            cp_async_4(ptx::smem_u32(&meta[slot].ks[lane >> 4]), a.k_scales + ph);
+                            cp_async_4(ptx::smem_u32(&meta[slot].vs[lane >> 4]), a.v_scales + ph);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < C::CHUNKS; ++i) {
+                        const int p = i * 32 + lane, r = p / C::CHUNKS, c = p % C::CHUNKS;
+                        const bool yes = (vis >> r) & 1u;
+                        const uint32_t at = dst + r * C::ROW + swizzled<C::CHUNKS>(r, c) * 16;
+                        size_t ko = 0, vo = 0;
+                        if constexpr (DENSE) {
+                            ko = (size_t)(n0 + r) * a.ks[2] * 2 + c * 16;
+                            vo = (size_t)(n0 + r) * a.vs[2] * 2 + c * 16;
+                        } else {
+                            const int id = __shfl_sync(0xffffffffu, ahead, r);
+                            ko = vo = (((size_t)id * a.Hk + g) * a.page + (n0 + r) % a.page) * D + c * 16;
+                        }
+                        cp_async_16_or_zero(at, yes ? kbase + ko : kbase, yes);
+                        cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vbase + vo : vbase, yes);
+                    }
+                }
+                ahead = look_ahead(it + 1);
+            }
+            ptx::cp_async_commit();
+        };
+#pragma unroll
+        for (int s = 0; s < C::STAGES - 1; ++s) issue(s);
+
+        // -------------------------------------------------------------------- tiles of 32 keys
+        for (int it = 0; t0 + warp + it * kWarps < t1; ++it) {
+            issue(it + C::STAGES - 1);
+            ptx::cp_async_wait_group<C::STAGES - 1>();
+            __syncwarp();
+            const int slot = it % C::STAGES, n0 = (t0 + warp + it * kWarps) * kKeys;
+            const uint32_t kt = ring + slot * C::STAGE, vt = kt + kKeys * C::ROW;
+            const unsigned vis = meta[slot].vis;
+            if (vis != 0) {
+                // ------ scores
+                float s[4][4];
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) {
+                    const int r = nt * 8 + gq;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[nt][x] = 0.0f;
+                    if constexpr (C::ROW / 4 >= 16) {
+#pragma unroll
+                        for (int c = 0; c < C::CHUNKS / 4; ++c) {
+                            uint32_t w[4];
+                            lds<16>(kt + r * C::ROW + swizzled<C::CHUNKS>(r, c * 4 + t4) * 16, w);
+                            if constexpr (DENSE) {
+                                mma16<MMA_BF16>(s[nt], qf[c * 2], w[0], w[1]);
+                                mma16<MMA_BF16>(s[nt], qf[c * 2 + 1], w[2], w[3]);
+                            } else {
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    uint32_t p01, p23;
+                                    codes_to_f16<I8>(w[x], p01, p23);
+                                    mma16<false>(s[nt], qf[c * 4 + x], p01, p23);
+                                }
+                            }
+                        }
+                    } else {
+                        constexpr int BYTES = C::ROW / 4;        // 8 or 4
+                        const int off = t4 * BYTES;
+                        uint32_t w[2];
+                        lds<BYTES>(kt + r * C::ROW + swizzled<C::CHUNKS>(r, off / 16) * 16 + off % 16, w);
+                        if constexpr (DENSE) mma16<MMA_BF16>(s[nt], qf[0], w[0], w[1]);
+                        else {
+#pragma unroll
+                            for (int x = 0; x < BYTES / 4; ++x) {
+                                uint32_t p01, p23;
+                                codes_to_f16<I8>(w[x], p01, p23);
+                                mma16<false>(s[nt], qf[x], p01, p23);
+                            }
+                        }
+                    }
+                }
+                // ------ softmax: element (row gq + 8 * (x >> 1), key nt * 8 + 2 t4 + (x & 1))
+                float sc[2][2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if constexpr (DENSE) sc[half][u] = rscale[half];
+                        else sc[half][u] = rscale[half] * meta[slot].ks[a.page == 16 ? u : 0];
+                    }
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int n = nt * 8 + 2 * t4 + (x & 1), half = x >> 1;
+                        const bool ok = ((vis >> n) & 1u) && n0 + n < last[half];
+                        s[nt][x] = ok ? s[nt][x] * sc[half][nt >> 1] : -INFINITY;
+                        top[half] = fmaxf(top[half], s[nt][x]);
+                    }
+                float keep[2], ref[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
+                    top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
+                    const float now = fmaxf(m[half], top[half]);
+                    ref[half] = now == -INFINITY ? 0.0f : now;
+                    keep[half] = exp2_fast(m[half] - ref[half]);
+                    m[half] = now;
+                    l[half] *= keep[half];
+                }
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        s[nt][x] = exp2_fast(s[nt][x] - ref[x >> 1]);
+                        l[x >> 1] += s[nt][x];
+                    }
+                if (__any_sync(0xffffffffu, keep[0] != 1.0f || keep[1] != 1.0f)) {
+#pragma unroll
+                    for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[j][x] *= keep[x >> 1];
+                }
+                uint32_t p[2][4], q[2][4];
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float lo = s[2 * kk + (x >> 1)][(x & 1) * 2], hi = s[2 * kk + (x >> 1)][(x & 1) * 2 + 1];
+                        p[kk][x] = pack2<MMA_BF16>(lo, hi);
+                        if constexpr (SPLIT_P) {
+                            const float2 f = unpack2<MMA_BF16>(p[kk][x]);
+                            q[kk][x] = pack2<MMA_BF16>(lo - f.x, hi - f.y);
+                        }
+                    }
+                // ------ values: column gq * (D / 8) + j is the MMA's column gq of tile j
+                constexpr int VB = D / 8 * C::ESIZE;                        // bytes of a key that a lane takes
+                constexpr int PIECE = VB < 16 ? VB : 16, WORDS = VB < 4 ? 1 : VB / 4;
+                uint32_t v[2][4][WORDS];
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int r = kk * 16 + 2 * t4 + (x & 1) + (x >> 1) * 8;
+#pragma unroll
+                        for (int y = 0; y < VB / PIECE; ++y) {
+                            const int off = gq * VB + y * PIECE;
+                            lds<PIECE>(vt + r * C::ROW + swizzled<C::CHUNKS>(r, off / 16) * 16 + off % 16, &v[kk][x][y * 4]);
+                        }
+                    }
+                if constexpr (DENSE) {
+#pragma unroll
+                    for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+                        for (int kk = 0; kk < 2; ++kk) {
+                            const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
+                            const uint32_t b0 = __byte_perm(v[kk][0][j / 2], v[kk][1][j / 2], sel), b1 = __byte_perm(v[kk][2][j / 2], v[kk][3][j / 2], sel);
+                            mma16<MMA_BF16>(o[j], p[kk], b0, b1);
+                            mma16<MMA_BF16>(o[j], q[kk], b0, b1);
+                        }
+                } else {
+                    // a row that sees nothing of a page takes nothing of its scale either, which may not be a number
+                    float vs[2][2];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) vs[half][u] = n0 + u * 16 < last[half] && ((vis >> (u * 16)) & 0xffffu) ? meta[slot].vs[a.page == 16 ? u : 0] : 0.0f;
+#pragma unroll
+                    for (int jw = 0; jw < (NTILES + 3) / 4; ++jw) {
+                        float tmp[4][4];
+#pragma unroll
+                        for (int kk = 0; kk < 2; ++kk) {
+                            uint32_t b0[4], b1[4];
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                uint32_t* bb = y ? b1 : b0;
+                                uint32_t w0 = v[kk][2 * y][jw], w1 = v[kk][2 * y + 1][jw];
+                                if constexpr (I8) { w0 ^= 0x80808080u; w1 ^= 0x80808080u; }
+                                const uint32_t lo = __byte_perm(w0, w1, 0x5140), hi = __byte_perm(w0, w1, 0x7362);   // (a0 b0 a1 b1), (a2 b2 a3 b3)
+                                if constexpr (I8) {
+                                    bb[0] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4140));
+                                    bb[1] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4342));
+                                    bb[2] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4140));
+                                    bb[3] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4342));
+                                } else {
+                                    bb[0] = e4m3x2_to_f16x2(lo);
+                                    bb[1] = e4m3x2_hi_to_f16x2(lo);
+                                    bb[2] = e4m3x2_to_f16x2(hi);
+                                    bb[3] = e4m3x2_hi_to_f16x2(hi);
+                                }
+                            }
+#pragma unroll
+                            for (int jj = 0; jj < 4; ++jj) {
+                                const int j = jw * 4 + jj;
+                                if (j >= NTILES) continue;
+                                if (kk == 0 || a.page == 16) tmp[jj][0] = tmp[jj][1] = tmp[jj][2] = tmp[jj][3] = 0.0f;
+                                mma16<false>(tmp[jj], p[kk], b0[jj], b1[jj]);
+                                if constexpr (SPLIT_P) mma16<false>(tmp[jj], q[kk], b0[jj], b1[jj]);
+                                if (kk == 1 || a.page == 16) {
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) o[j][x] = fmaf(tmp[jj][x], vs[x >> 1][kk == 1 && a.page != 16 ? 0 : kk], o[j][x]);
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        ptx::cp_async_wait_all();
+        // -------------------------------------------------------------------- the four warps' parts
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
+            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+        }
+        __syncthreads();                       // every ring has been read
+        float* so = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = gq + half * 8;
+            if (t4 == 0) { s_m[warp][r] = m[half]; s_l[warp][r] = l[half]; }
+#pragma unroll
+            for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) so[(warp * kRowTile + r) * D + (2 * t4 + x) * (D / 8) + j] = o[j][half * 2 + x];
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < kRowTile * D / 2; e += kWarps * 32) {
+            const int r = e / (D / 2), c = e % (D / 2) * 2, row = row0 + r;
+            if (row >= rows) break;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = exp2_fast(s_m[w][r] - ref);
+                sum += s_l[w][r] * f;
+                x += so[(w * kRowTile + r) * D + c] * f;
+                y += so[(w * kRowTile + r) * D + c + 1] * f;
+            }
+            const size_t out = ((size_t)b * a.k_h + s_pos[row / a.Tq]) * a.Tq + row % a.Tq;
+            if (n_splits == 1) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                reinterpret_cast<uint32_t*>(a.O)[(out * D + c) / 2] = pack2<BF16>(sum == 0.0f ? 0.0f : x * inv, sum == 0.0f ? 0.0f : y * inv);
+            } else {
+                const size_t at = (size_t)split * a.B * a.k_h * a.Tq + out;
+                *reinterpret_cast<float2*>(part + at * D + c) = make_float2(x, y);
+                if (c == 0) ml[at] = make_float2(top, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the parts of a split axis: a warp per row.
+template <bool BF16>
+__global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int n_splits) {
+    const int lane = threadIdx.x & 31;
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    if (row >= rows) return;
+    const int j = (int)(row / a.Tq % a.k_h), b = (int)(row / a.Tq / a.k_h);
+    if (kv_head(a, b, j) < 0) return;         // (its zero rows are written)
+    float top = -INFINITY;
+    for (int s = lane; s < n_splits; s += 32) top = fmaxf(top, ml[s * rows + row].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float acc[4] = {}, sum = 0.0f;
+    const int cols = a.d / 32 ? a.d / 32 : 1, c0 = lane * cols;
+    for (int s = 0; s < n_splits; ++s) {
+        const float2 x = ml[s * rows + row];
+        const float f = exp2_fast(x.x - ref);
+        sum += x.y * f;
+        if (x.x == -INFINITY && x.y == 0.0f) continue;    // (nothing seen there)
+        if (c0 < a.d)
+            for (int c = 0; c < cols; ++c) acc[c] += part[(s * rows + row) * a.d + c0 + c] * f;
+    }
+    if (c0 < a.d)
+        for (int c = 0; c < cols; ++c) {
+            const float v = sum == 0.0f ? 0.0f : acc[c] / sum;
+            if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(a.O)[row * a.d + c0 + c] = __float2bfloat16_rn(v);
+            else reinterpret_cast<__half*>(a.O)[row * a.d + c0 + c] = __float2half_rn(v);
+        }
+}
+
+// Blocks along the keys: enough to fill the GPU twice over, each with a tile for every warp at least.
+int rows_splits(const KvAttendArgs& a) {
+    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
+    const long long row_tiles = ((long long)heads * a.Tq + kRowTile - 1) / kRowTile;
+    const long long blocks = (long long)a.B * a.Hk * (row_tiles < 64 ? row_tiles : 64);
+    const long long most = ((long long)a.Tk + kWarps * kKeys - 1) / (kWarps * kKeys);
+    if (blocks == 0) return 1;
+    long long n = (2 * kSmCount + blocks - 1) / blocks;
+    if (n > most) n = most;
+    if (n > 128) n = 128;
+    return n < 1 ? 1 : (int)n;
+}
+
+template <int KV, int D, bool BF16>
+int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    using C = RowsCfg<KV, D>;
+    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
+    const long long row_tiles = ((long long)heads * a.Tq + kRowTile - 1) / kRowTile;
+    const int n_splits = rows_splits(a);
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
+    float* part = nullptr;
+    float2* ml = nullptr;
+    if (n_splits > 1) {
+        part = ws.take<float>(n_splits * rows * D);
+        ml = ws.take<float2>(n_splits * rows);
+        if (!ws.ok) return SENTRY_ERR_WORKSPACE;
+    }
+    auto k = kv_rows_kernel<KV, D, BF16>;
+    SENTRY_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    {
+        LaunchScope ls(ctx, KS_KV_ATTEND, st);
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)(row_tiles < 64 ? row_tiles : 64)), dim3(kWarps * 32), C::SMEM, st, a,
+                                       part, ml, n_splits));
+    }
+    if (n_splits > 1) {
+        LaunchScope ls(ctx, KS_KV_COMBINE, st);
+        SENTRY_CUDA_TRY(launch_chained(kv_combine_kernel<BF16>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a, (const float*)part, (const float2*)ml, n_splits));
+    }
+    return SENTRY_OK;
+}
+
+template <int KV, bool BF16>
+int launch_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    switch (a.d) {
+        case 16: return launch_rows<KV, 16, BF16>(ctx, a, ws, st);
+        case 32: return launch_rows<KV, 32, BF16>(ctx, a, ws, st);
+        case 64: return launch_rows<KV, 64, BF16>(ctx, a, ws, st);
+        default: return launch_rows<KV, 128, BF16>(ctx, a, ws, st);
+    }
+}
+
+}  // namespace
+
+size_t kv_rows_ws_bytes(const KvAttendArgs& a) {
+    const int n = rows_splits(a);
+    if (n <= 1) return 0;
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
+    return align_up(n * rows * a.d * sizeof(float), 256) + n * rows * sizeof(float2) + 512;
+}
+
+int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    const bool bf16 = a.dtype == SENTRY_BF16;
+    if (a.format == 0) return bf16 ? launch_d<KV_BF16, true>(ctx, a, ws, st) : launch_d<KV_F16, false>(ctx, a, ws, st);
+    if (a.format == SENTRY_FP8_E4M3) return bf16 ? launch_d<KV_E4M3, true>(ctx, a, ws, st) : launch_d<KV_E4M3, false>(ctx, a, ws, st);
+    return bf16 ? launch_d<KV_I8, true>(ctx, a, ws, st) : launch_d<KV_I8, false>(ctx, a, ws, st);
+}

@@ -1,0 +1,94 @@
+// Declarations shared by the serving operators (8-bit linear layer, cross attention, 8-bit cache): argument structs, launchers and
+// the integer rounding that two of them use.
+#pragma once
+#include "common.cuh"
+
+constexpr int kServeMaxHeads = 256;
+
+// Attention of packed rows over a dense tensor (format 0) or a paged 8-bit cache.
+struct KvAttendArgs {
+    int B, Tq, Tk;              // Tk: keys per sample (dense), or the capacity max_pages * page
+    int Hq, Hk, d, k_h, dtype;
+    long long qs[3], ks[3], vs[3];   // strides in elements: batch, head, token
+    const void *Q, *K, *V;
+    void* O;
+    const int32_t *kept, *ids, *lengths;
+    const uint32_t* masks;
+    int format, page, n_pages, max_pages, causal;
+    const float *k_scales, *v_scales;
+    const int32_t* table;
+    unsigned int* status;
+    int sm_count;
+};
+int launch_kv_generic(sentry_ctx* ctx, const KvAttendArgs& a, cudaStream_t st);            // fp32 rows
+size_t kv_rows_ws_bytes(const KvAttendArgs& a);
+int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);   // 16-bit rows, few of them
+
+struct AppendArgs {
+    sentry_kv_cache c;
+    sentry_append_desc d;
+    long long ks[3], vs[3];
+    const void *K, *V;
+    const int32_t *ids, *token_lengths, *lengths;
+    const uint32_t* masks;
+    int32_t* new_lengths;
+    unsigned int* status;
+};
+int launch_cache_append(sentry_ctx* ctx, const AppendArgs& a, cudaStream_t st);
+
+int launch_quantize_rows_i8(sentry_ctx* ctx, int M, int K, int dtype, const void* X, int8_t* codes, float* scales, cudaStream_t st);
+struct LinearArgs {
+    sentry_linear_desc d;
+    const int8_t *X, *W;
+    const float *xs, *ws, *bias;
+    void* Y;
+    unsigned int* status;
+};
+int launch_linear_i8(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st);
+
+#ifdef __CUDACC__
+// x / s to the nearest integer, ties to even, of the exact quotient; |x| <= 127 s (1 + 2^-22), s >= 2^-126, inv = 1 / s rounded.
+// The product with the rounded reciprocal is at most one off; x - r s is exact (a multiple of the smaller operand's last place, below
+// s in size), and twice it against s says which neighbour is nearer.
+__device__ __forceinline__ int round_quotient_i8(float x, float s, float inv) {
+    float r = rintf(x * inv);
+    const float e2 = 2.0f * fmaf(-r, s, x);
+    const bool odd = ((int)r) & 1;
+    if (e2 > s || (e2 == s && odd)) r += 1.0f;
+    else if (e2 < -s || (e2 == -s && odd)) r -= 1.0f;
+    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
+}
+__device__ __forceinline__ uint32_t pack_i8x4(int a, int b, int c, int d) {
+    return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)(d & 255) << 24);
+}
+// (the product with 1/127 rounded to fp32, not the quotient: what the header defines)
+__device__ __forceinline__ float scale_i8(float top) { return top > 0.0f ? fmaxf(__fmul_rn(top, 1.0f / 127.0f), 1.17549435e-38f) : 0.0f; }
+
+// Sixteen bytes of a 16-bit or fp32 tensor as floats.
+template <typename T> struct Vec16;
+template <> struct Vec16<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void get(const uint4& v, float* f) {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+};
+template <> struct Vec16<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void get(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+};
+template <> struct Vec16<__half> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void get(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __half2float(__ushort_as_half((unsigned short)(w[i] & 0xffffu)));
+            f[2 * i + 1] = __half2float(__ushort_as_half((unsigned short)(w[i] >> 16)));
+        }
+    }
+};
+#endif
