@@ -17,7 +17,7 @@ int strides_of(const int64_t given[3], int H, int T, int d, int dtype, long long
     const int unit = dtype == SENTRY_F32 ? 4 : 8;
     for (int i = 0; i < 3; ++i) {
         if (given[i] < 0) return SENTRY_ERR_BAD_SHAPE;
-        if (given[i] % unit != 0 || given[i] > (1LL << 46)) return SENTRY_ERR_UNSUPPORTED;
+        if (given[i] % unit != 0 || given[i] > (1LL << 38)) return SENTRY_ERR_UNSUPPORTED;
         out[i] = given[i];
     }
     return SENTRY_OK;
@@ -72,7 +72,7 @@ int cache_args(const sentry_kv_cache* c, const sentry_cache_attend_desc* d, KvAt
     return strides_of(d->q_stride, d->Hq, d->Tq, c->d, d->dtype, a.qs);
 }
 
-size_t kv_ws_bytes(const KvAttendArgs& a) { return a.dtype == SENTRY_F32 ? 0 : kv_rows_ws_bytes(a); }
+size_t kv_ws_bytes(const KvAttendArgs& a) { return a.dtype == SENTRY_F32 ? 0 : kv_tc_takes(a) ? kv_tc_ws_bytes(a) : kv_rows_ws_bytes(a); }
 
 int run_attend(sentry_ctx* ctx, KvAttendArgs& a, cudaStream_t st) {
     ctx->last_launches = 0;
@@ -82,7 +82,7 @@ int run_attend(sentry_ctx* ctx, KvAttendArgs& a, cudaStream_t st) {
     SENTRY_ON_DEVICE(ctx->device);
     if (a.dtype == SENTRY_F32) return launch_kv_generic(ctx, a, st);
     WsAlloc ws(ctx->workspace, ctx->workspace_bytes);
-    return launch_kv_rows(ctx, a, ws, st);
+    return kv_tc_takes(a) ? launch_kv_tc(ctx, a, ws, st) : launch_kv_rows(ctx, a, ws, st);
 }
 
 }  // namespace

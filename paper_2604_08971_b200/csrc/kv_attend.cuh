@@ -24,3 +24,38 @@ __device__ __forceinline__ float code_value(uint8_t c) {
         return __half2float(__half(h));
     }
 }
+
+// The positions of sample b's list whose head belongs to group g, in the list's order; by one warp.  With `first`, positions that hold no
+// head get their zero rows here, and the status bit.
+__device__ __forceinline__ int kv_group_heads(const KvAttendArgs& a, int b, int g, bool first, short* head, short* pos) {
+    const int lane = threadIdx.x & 31, per = a.Hq / a.Hk;
+    int n = 0;
+    for (int j0 = 0; j0 < a.k_h; j0 += 32) {
+        const int j = j0 + lane, h = j < a.k_h ? kv_head(a, b, j) : -2;
+        const unsigned mine = __ballot_sync(0xffffffffu, h >= 0 && h / per == g);
+        if ((mine >> lane) & 1u) {
+            const int at = n + __popc(mine & ((1u << lane) - 1u));
+            head[at] = (short)h;
+            pos[at] = (short)j;
+        }
+        n += __popc(mine);
+        for (unsigned none = __ballot_sync(0xffffffffu, first && h == -1); none; none &= none - 1) {
+            if (lane == 0) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+            uint32_t* o = (uint32_t*)a.O + ((size_t)b * a.k_h + j0 + __ffs(none) - 1) * a.Tq * (a.d / 2);
+            for (size_t e = lane; e < (size_t)a.Tq * (a.d / 2); e += 32) o[e] = 0u;
+        }
+    }
+    return n;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t v;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
+    return v;
+}

@@ -66,18 +66,6 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t v;
-    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
-    return v;
-}
 template <bool BF16>
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
     if constexpr (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
@@ -137,23 +125,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
 
     // the kept heads of this group, in the list's order
     if (warp == 0) {
-        const int per = a.Hq / a.Hk;
-        int n = 0;
-        for (int j0 = 0; j0 < a.k_h; j0 += 32) {
-            const int j = j0 + lane, h = j < a.k_h ? kv_head(a, b, j) : -2;
-            const unsigned mine = __ballot_sync(0xffffffffu, h >= 0 && h / per == g);
-            if ((mine >> lane) & 1u) {
-                const int at = n + __popc(mine & ((1u << lane) - 1u));
-                s_head[at] = (short)h;
-                s_pos[at] = (short)j;
-            }
-            n += __popc(mine);
-            if (h == -1 && g == 0 && split == 0 && blockIdx.y == 0) {   // not a head: zero rows
-                atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
-                uint32_t* o = (uint32_t*)a.O + ((size_t)b * a.k_h + j) * a.Tq * (D / 2);
-                for (size_t e = 0; e < (size_t)a.Tq * (D / 2); ++e) o[e] = 0u;
-            }
-        }
+        const int n = kv_group_heads(a, b, g, g == 0 && split == 0 && blockIdx.y == 0, s_head, s_pos);
         if (lane == 0) s_heads = n;
     }
     __syncthreads();
@@ -514,38 +486,6 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
     }
 }
 
-// Joins the parts of a split axis: a warp per row.
-template <bool BF16>
-__global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int n_splits) {
-    const int lane = threadIdx.x & 31;
-    const size_t rows = (size_t)a.B * a.k_h * a.Tq, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    grid_dependency_wait();
-    if (row >= rows) return;
-    const int j = (int)(row / a.Tq % a.k_h), b = (int)(row / a.Tq / a.k_h);
-    if (kv_head(a, b, j) < 0) return;         // (its zero rows are written)
-    float top = -INFINITY;
-    for (int s = lane; s < n_splits; s += 32) top = fmaxf(top, ml[s * rows + row].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float acc[4] = {}, sum = 0.0f;
-    const int cols = a.d / 32 ? a.d / 32 : 1, c0 = lane * cols;
-    for (int s = 0; s < n_splits; ++s) {
-        const float2 x = ml[s * rows + row];
-        const float f = exp2_fast(x.x - ref);
-        sum += x.y * f;
-        if (x.x == -INFINITY && x.y == 0.0f) continue;    // (nothing seen there)
-        if (c0 < a.d)
-            for (int c = 0; c < cols; ++c) acc[c] += part[(s * rows + row) * a.d + c0 + c] * f;
-    }
-    if (c0 < a.d)
-        for (int c = 0; c < cols; ++c) {
-            const float v = sum == 0.0f ? 0.0f : acc[c] / sum;
-            if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(a.O)[row * a.d + c0 + c] = __float2bfloat16_rn(v);
-            else reinterpret_cast<__half*>(a.O)[row * a.d + c0 + c] = __float2half_rn(v);
-        }
-}
-
 // Blocks along the keys: enough to fill the GPU twice over, each with a tile for every warp at least.
 int rows_splits(const KvAttendArgs& a) {
     const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
@@ -581,8 +521,7 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
                                        part, ml, n_splits));
     }
     if (n_splits > 1) {
-        LaunchScope ls(ctx, KS_KV_COMBINE, st);
-        SENTRY_CUDA_TRY(launch_chained(kv_combine_kernel<BF16>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a, (const float*)part, (const float2*)ml, n_splits));
+        return launch_kv_combine(ctx, a, part, ml, n_splits, st);
     }
     return SENTRY_OK;
 }

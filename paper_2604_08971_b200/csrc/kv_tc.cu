@@ -1,0 +1,474 @@
+// Cross attention of many rows on the 5th-generation tensor cores (16-bit types).
+//
+// The rows of a KV group (kept heads x Tq) are packed; a CTA takes two tiles of 128 of them and walks the keys 128 at a time:
+//   S_t = Q_t K^T        tcgen05, both operands in shared memory (128-byte rows, swizzled), S in tensor memory
+//   P_t = 2^(S c - m c)  a thread is a row: it reads its 128 scores, keeps its running maximum and sum, and writes the weights in 16 bits over
+//                        the scores that it has read
+//   O_t += P_t V         tcgen05, P from tensor memory, V as it lies in memory (MN-major)
+// Two tiles, so that the tensor core works for one while the other's rows are exponentiated.  The accumulator follows the running maximum
+// only where it grew by more than 2^8: until then weights are up to 2^8 instead of 1, which costs neither range nor precision, and
+// almost no iteration touches O.
+// K and V come by TMA where 128 present keys follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
+// where they do not: the last tile of a sample, and tiles across the border of a missing modality.
+// Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
+#include <cuda.h>
+
+#include "kv_attend.cuh"
+#include "tc_common.cuh"
+
+namespace {
+
+constexpr int kTM = 128, kTN = 128;          // rows of a tile, keys of a step
+constexpr int kTcThreads = 384;              // two softmax groups of four warps, three loading warps, one issuer
+constexpr int kLoadWarp0 = 8, kLoadWarps = 3, kIssueWarp = 11;
+constexpr float kTcLog2e = 1.4426950408889634f;
+
+template <int D>
+struct TcCfg {
+    static constexpr int RB = D >= 64 ? 128 : D * 2;         // bytes of a shared-memory row (64 elements at most)
+    static constexpr int SLABS = D * 2 / RB;                 // column slabs of a tile
+    static constexpr int SLAB = 128 * RB;
+    static constexpr int TILE = SLABS * SLAB;                // 128 rows of D elements
+    static constexpr int STAGES = D == 128 ? 2 : 4;          // of K, and of V
+    static constexpr int SMEM = 2 * TILE + 2 * STAGES * TILE + 1024;
+};
+struct TcMisc {
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint32_t tmem_base;
+    int abort_flag;
+    int n_heads;
+    short head[kServeMaxHeads], pos[kServeMaxHeads];
+};
+
+// 16-byte piece c of row r in a tile of rows of RB bytes, swizzled in that row width's mode
+template <int RB>
+__device__ __forceinline__ uint32_t tile_offset(int r, int c) {
+    constexpr int PER = RB / 16;                   // pieces of a row
+    const int f = RB == 128 ? r & 7 : RB == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+    return (uint32_t)((c / PER) * (128 * RB) + r * RB + (((c % PER) ^ f) << 4));
+}
+
+struct TcMaps { CUtensorMap k, v; };
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+                 : "memory");
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kTcThreads, 1)
+kv_tc_kernel(const __grid_constant__ TcMaps maps, const KvAttendArgs a, const int32_t* __restrict__ list, const int32_t* __restrict__ counts,
+             float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
+    using C = TcCfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ TcMisc misc_s;
+    TcMisc* misc = &misc_s;
+    volatile int* abort_flag = &misc->abort_flag;
+    const uint32_t q_smem = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t k_smem = q_smem + 2 * C::TILE, v_smem = k_smem + C::STAGES * C::TILE;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = blockIdx.x % n_splits, bg = blockIdx.x / n_splits, b = bg / a.Hk, g = bg % a.Hk;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&misc->k_full[s]), kLoadWarps);
+            ptx::mbar_init(ptx::smem_u32(&misc->k_empty[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&misc->v_full[s]), kLoadWarps);
+            ptx::mbar_init(ptx::smem_u32(&misc->v_empty[s]), 1);
+        }
+        for (int t = 0; t < 2; ++t) {
+            ptx::mbar_init(ptx::smem_u32(&misc->s_full[t]), 1);
+            ptx::mbar_init(ptx::smem_u32(&misc->p_full[t]), 4);
+            ptx::mbar_init(ptx::smem_u32(&misc->o_full[t]), 1);
+        }
+        misc->abort_flag = 0;
+        ptx::fence_barrier_init();
+        ptx::prefetch_tensormap(&maps.k);
+        ptx::prefetch_tensormap(&maps.v);
+    }
+    grid_dependency_wait();
+    if (warp == 0) {
+        const int n = kv_group_heads(a, b, g, g == 0 && split == 0 && blockIdx.y == 0, misc->head, misc->pos);
+        if (lane == 0) misc->n_heads = n;
+    }
+    __syncthreads();
+    const int rows = misc->n_heads * a.Tq;
+    if ((int)blockIdx.y * 2 * kTM >= rows) return;
+    if (warp == kIssueWarp) {
+        ptx::tmem_alloc(ptx::smem_u32(&misc->tmem_base), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = misc->tmem_base;
+
+    // present keys of the sample, in order: those of the list, or the first `count`
+    const int32_t* at = list ? list + (size_t)b * a.Tk : nullptr;
+    const int count = list ? counts[b] : kv_length(a, b);
+    const int tiles = (count + kTN - 1) / kTN, per_split = (tiles + n_splits - 1) / n_splits;
+    const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles), steps = t1 - t0;
+    uint32_t done = 0;                            // steps of the row blocks before
+
+    for (int rb = blockIdx.y; rb * 2 * kTM < rows; rb += gridDim.y, done += (uint32_t)steps) {
+        const int row0 = rb * 2 * kTM;
+        const int halves = rows - row0 > kTM ? 2 : 1;
+        if (steps > 0) {
+            // ---------------------------------------------------------------- Q: all threads
+            for (int e = threadIdx.x; e < halves * kTM * (D / 8); e += kTcThreads) {
+                const int r = e / (D / 8), c = e % (D / 8), row = row0 + r;
+                const uint32_t dst = q_smem + (r >> 7) * C::TILE + tile_offset<C::RB>(r & 127, c);
+                if (row < rows) {
+                    const long long src = b * a.qs[0] + misc->head[row / a.Tq] * a.qs[1] + row % a.Tq * a.qs[2] + c * 8;
+                    ptx::cp_async_16(dst, (const uint16_t*)a.Q + src);
+                } else {
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
+                }
+            }
+            ptx::cp_async_wait_all();
+            ptx::fence_proxy_async_smem();
+            __syncthreads();
+        }
+        if (warp >= kLoadWarp0 && warp < kLoadWarp0 + kLoadWarps) {
+            // ---------------------------------------------------------------- K and V
+            const int lw = warp - kLoadWarp0;
+            const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
+            bool ok = true;
+            for (int j = 0; j < steps && ok; ++j) {
+                const uint32_t n = done + j, s = n % C::STAGES, use = n / C::STAGES;
+                const int p0 = (t0 + j) * kTN;
+                const bool full = p0 + kTN <= count;
+                const int first = at ? at[p0] : p0;
+                const bool together = full && (at == nullptr || at[p0 + kTN - 1] - first == kTN - 1);
+#pragma unroll 1
+                for (int is_v = 0; is_v < 2 && ok; ++is_v) {
+                    uint64_t* full_bar = is_v ? &misc->v_full[s] : &misc->k_full[s];
+                    ok = warp_wait(is_v ? &misc->v_empty[s] : &misc->k_empty[s], (use & 1) ^ 1, abort_flag);
+                    if (!ok) break;
+                    const uint32_t dst = (is_v ? v_smem : k_smem) + s * C::TILE;
+                    if (together) {
+                        if (lw == 0) {
+                            if (elect_one()) {
+                                const uint32_t bar = ptx::smem_u32(full_bar);
+                                ptx::mbar_arrive_expect_tx(bar, C::TILE);
+#pragma unroll
+                                for (int c = 0; c < C::SLABS; ++c)
+                                    tma_load_4d(dst + c * C::SLAB, is_v ? &maps.v : &maps.k, c * 64, first, is_v ? vg : kg, is_v ? vb : kb, bar);
+                            }
+                            __syncwarp();
+                        } else {
+                            warp_arrive(full_bar);
+                        }
+                    } else {
+                        const long long* st = is_v ? a.vs : a.ks;
+                        const uint16_t* src = (const uint16_t*)(is_v ? a.V : a.K) + b * st[0] + g * st[1];
+                        for (int e = lw * 32 + lane; e < kTN * (D / 8); e += kLoadWarps * 32) {
+                            const int r = e / (D / 8), c = e % (D / 8);
+                            const uint32_t to = dst + tile_offset<C::RB>(r, c);
+                            if (p0 + r < count) ptx::cp_async_16(to, src + (at ? at[p0 + r] : p0 + r) * st[2] + c * 8);
+                            else asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+                        }
+                        ptx::cp_async_wait_all();
+                        ptx::fence_proxy_async_smem();
+                        warp_arrive(full_bar);
+                    }
+                }
+            }
+        } else if (warp == kIssueWarp) {
+            // ---------------------------------------------------------------- UMMAs
+            constexpr uint32_t qk = BF16 ? ptx::umma_idesc_bf16(kTM, kTN) : ptx::umma_idesc_f16(kTM, kTN);
+            constexpr uint32_t pv = BF16 ? ptx::umma_idesc_bf16_major(kTM, D, false, true) : ptx::umma_idesc_f16_major(kTM, D, false, true);
+            bool ok = true;
+            auto scores = [&](int t, uint32_t s) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (k * 32 / C::RB) * C::SLAB + k * 32 % C::RB;
+                    ptx::umma_bf16(tmem + t * kTN, ptx::umma_smem_desc_rows(q_smem + t * C::TILE + off, C::RB),
+                                   ptx::umma_smem_desc_rows(k_smem + s * C::TILE + off, C::RB), qk, k > 0 ? 1u : 0u);
+                }
+                ptx::umma_commit(ptx::smem_u32(&misc->s_full[t]));
+            };
+            if (steps > 0) {
+                const uint32_t s = done % C::STAGES, use = done / C::STAGES;
+                ok = warp_wait(&misc->k_full[s], use & 1, abort_flag);
+                if (ok) {
+                    ptx::tc_fence_after_sync();
+                    if (elect_one()) {
+                        for (int t = 0; t < halves; ++t) scores(t, s);
+                        ptx::umma_commit(ptx::smem_u32(&misc->k_empty[s]));
+                    }
+                    __syncwarp();
+                }
+            }
+            for (int j = 0; j < steps && ok; ++j) {
+                const uint32_t n = done + j, s = n % C::STAGES, use = n / C::STAGES;
+                const uint32_t s2 = (n + 1) % C::STAGES, use2 = (n + 1) / C::STAGES;
+                const bool more = j + 1 < steps;
+                ok = warp_wait(&misc->v_full[s], use & 1, abort_flag);
+                for (int t = 0; t < halves && ok; ++t) {
+                    ok = warp_wait(&misc->p_full[t], n & 1, abort_flag);
+                    if (!ok) break;
+                    if (more && t == 0) ok = warp_wait(&misc->k_full[s2], use2 & 1, abort_flag);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kTN / 16; ++k)
+                            ptx::umma_bf16_tmem_a(tmem + 256 + t * D, tmem + t * kTN + k * 8,
+                                                  ptx::umma_smem_desc_rows(v_smem + s * C::TILE + k * 16 * C::RB, C::RB, C::SLAB), pv, (j > 0 || k > 0) ? 1u : 0u);
+                        ptx::umma_commit(ptx::smem_u32(&misc->o_full[t]));
+                        if (t == halves - 1) ptx::umma_commit(ptx::smem_u32(&misc->v_empty[s]));
+                        if (more) {
+                            scores(t, s2);
+                            if (t == halves - 1) ptx::umma_commit(ptx::smem_u32(&misc->k_empty[s2]));
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        } else if (warp < 8) {
+            // ---------------------------------------------------------------- softmax: a thread is a row
+            const int t = warp >> 2;
+            const int row = row0 + t * kTM + (warp & 3) * 32 + lane;
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+            const uint32_t sc = tmem + t * kTN + lanes, oc = tmem + 256 + t * D + lanes;
+            const float c = rsqrtf((float)D) * kTcLog2e;
+            // fp16 weights are taken 2^7 times as large (2^15 at most): its range is what small ones run out of
+            constexpr float kShift = BF16 ? 0.0f : 7.0f;
+            float m = -INFINITY, l = 0.0f;
+            bool ok = true;
+            for (int j = 0; j < steps && ok && t < halves; ++j) {
+                const uint32_t n = done + j;
+                ok = warp_wait(&misc->s_full[t], n & 1, abort_flag);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+                uint32_t s[kTN / 32][32];
+#pragma unroll
+                for (int x = 0; x < kTN / 32; ++x) ptx::tmem_ld_32x32(sc + x * 32, s[x]);
+                ptx::tmem_ld_wait();
+                const int valid = count - (t0 + j) * kTN;
+                if (valid < kTN) {
+#pragma unroll
+                    for (int x = 0; x < kTN; ++x)
+                        if (x >= valid) s[x / 32][x % 32] = 0xff800000u;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int x = 0; x < kTN; x += 8)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        top[y] = fmaxf(top[y], fmaxf(__uint_as_float(s[x / 32][x % 32 + 2 * y]), __uint_as_float(s[x / 32][x % 32 + 2 * y + 1])));
+                const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+                if (j == 0) m = now;
+                else {
+                    const bool grew = (now - m) * c > 8.0f;
+                    if (__any_sync(0xffffffffu, grew)) {
+                        // O follows the maximum; the last product into it has to be complete
+                        ok = warp_wait(&misc->o_full[t], (n - 1) & 1, abort_flag);
+                        if (!ok) break;
+                        ptx::tc_fence_after_sync();
+                        const float keep = m == now ? 1.0f : exp2_fast((m - now) * c);
+                        m = now;
+                        l *= keep;
+#pragma unroll
+                        for (int x = 0; x < D; x += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x16(oc + x, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
+                            ptx::tmem_st_32x16(oc + x, o);
+                        }
+                    }
+                }
+                const float mc = (m == -INFINITY ? 0.0f : m * c) - kShift;
+                float sum[4] = {};
+#pragma unroll
+                for (int x = 0; x < kTN / 32; ++x) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) {
+                        const float p0 = exp2_fast(fmaf(__uint_as_float(s[x][2 * y]), c, -mc)), p1 = exp2_fast(fmaf(__uint_as_float(s[x][2 * y + 1]), c, -mc));
+                        sum[y & 1] += p0;
+                        sum[2 + (y & 1)] += p1;
+                        w[y] = pack2<BF16>(p0, p1);
+                    }
+                    ptx::tmem_st_32x16(sc + x * 16, w);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before_sync();
+                warp_arrive(&misc->p_full[t]);
+            }
+            // ---------------------------------------------------------------- results
+            if (t < halves) {
+                if (steps > 0 && ok) ok = warp_wait(&misc->o_full[t], (done + steps - 1) & 1, abort_flag);
+                ptx::tc_fence_after_sync();
+                if (ok) {
+                    const bool in = row < rows;
+                    const size_t out = in ? ((size_t)b * a.k_h + misc->pos[row / a.Tq]) * a.Tq + row % a.Tq : 0;
+                    const size_t pat = (size_t)split * a.B * a.k_h * a.Tq + out;
+                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * c - kShift, l) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+                    for (int x = 0; x < D; x += 16) {
+                        uint32_t o[16];
+                        if (steps > 0) {
+                            ptx::tmem_ld_32x16(oc + x, o);
+                            ptx::tmem_ld_wait();
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) o[y] = 0u;
+                        }
+                        if (!in) continue;
+                        if (n_splits == 1) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int y = 0; y < 8; ++y)
+                                w[y] = l == 0.0f ? 0u : pack2<BF16>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
+                            uint4* dst = reinterpret_cast<uint4*>((uint16_t*)a.O + out * D + x);
+                            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                            dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                        } else if (steps > 0) {
+                            uint4* dst = reinterpret_cast<uint4*>(part + pat * D + x);
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) dst[y] = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+                        }
+                    }
+                }
+                ptx::tc_fence_before_sync();
+            }
+        }
+        __syncthreads();                      // Q and O may be taken over
+        ptx::tc_fence_after_sync();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicOr(a.status, SENTRY_STATUS_BIT_TIMEOUT);
+        const long long start = clock64();
+        while (clock64() - start < 2000000LL) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == kIssueWarp) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+// The present keys of every sample, in order: a block per sample.
+__global__ void __launch_bounds__(1024) kv_plan_kernel(const KvAttendArgs a, int32_t* __restrict__ list, int32_t* __restrict__ counts) {
+    __shared__ int s_warp[32];
+    const int b = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    grid_dependents_start_if_small();
+    grid_dependency_wait();
+    const int len = kv_length(a, b);
+    const uint32_t mask = a.masks[b];
+    int base = 0;
+    for (int n0 = 0; n0 < len; n0 += 1024) {
+        const int n = n0 + threadIdx.x;
+        const bool ok = n < len && kv_present(a.ids[n], mask);
+        const unsigned here = __ballot_sync(0xffffffffu, ok);
+        __syncthreads();
+        if (lane == 0) s_warp[warp] = __popc(here);
+        __syncthreads();
+        int before = base, all = 0;
+        for (int w = 0; w < 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
+        if (ok) list[(size_t)b * a.Tk + before + __popc(here & ((1u << lane) - 1u))] = n;
+        base += all;
+    }
+    if (threadIdx.x == 0) counts[b] = base;
+}
+
+// K or V as (64 columns, 128 tokens) boxes of (d, token, head, batch); a dimension of stride 0 is one that every index shares.
+bool make_map_kv(CUtensorMap* tm, const void* ptr, const KvAttendArgs& a, const long long st[3], bool bf16) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (fn == nullptr) return false;
+    const int rb = a.d >= 64 ? 128 : a.d * 2;
+    const CUtensorMapSwizzle sw = rb == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : rb == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+    cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.Tk, st[1] ? (cuuint64_t)a.Hk : 1, st[0] ? (cuuint64_t)a.B : 1};
+    cuuint64_t strides[3] = {(cuuint64_t)st[2] * 2, (cuuint64_t)(st[1] ? st[1] : 8) * 2, (cuuint64_t)(st[0] ? st[0] : 8) * 2};
+    cuuint32_t box[4] = {(cuuint32_t)rb / 2, kTN, 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int group_rows(const KvAttendArgs& a) {
+    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
+    const long long r = (long long)heads * a.Tq;
+    return r > 0x7fffffffLL ? 0x7fffffff : (int)r;
+}
+long long row_blocks(const KvAttendArgs& a) {
+    const long long n = ((long long)group_rows(a) + 2 * kTM - 1) / (2 * kTM);
+    return n > 65535 ? 65535 : n;
+}
+// Blocks along the keys: where the row blocks alone leave SMs idle, each with two steps at least.
+int tc_splits(const KvAttendArgs& a) {
+    const long long units = (long long)a.B * a.Hk * row_blocks(a);
+    const long long tiles = ((long long)a.Tk + kTN - 1) / kTN;
+    if (units == 0) return 1;
+    long long n = kSmCount / units;
+    if (n > tiles / 2) n = tiles / 2;
+    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
+template <int D, bool BF16>
+int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    TcMaps maps;
+    if (!make_map_kv(&maps.k, a.K, a, a.ks, BF16) || !make_map_kv(&maps.v, a.V, a, a.vs, BF16)) return SENTRY_ERR_CUDA;
+    const int n_splits = tc_splits(a);
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
+    float* part = nullptr;
+    float2* ml = nullptr;
+    int32_t *list = nullptr, *counts = nullptr;
+    if (n_splits > 1) {
+        part = ws.take<float>(n_splits * rows * D);
+        ml = ws.take<float2>(n_splits * rows);
+    }
+    if (a.ids != nullptr) {
+        list = ws.take<int32_t>((size_t)a.B * a.Tk);
+        counts = ws.take<int32_t>(a.B);
+    }
+    if (!ws.ok) return SENTRY_ERR_WORKSPACE;
+    if (a.ids != nullptr) {
+        LaunchScope ls(ctx, KS_KV_PLAN, st);
+        SENTRY_CUDA_TRY(launch_chained(kv_plan_kernel, dim3((unsigned)a.B), dim3(1024), 0, st, a, list, counts));
+    }
+    auto k = kv_tc_kernel<D, BF16>;
+    SENTRY_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<D>::SMEM));
+    {
+        LaunchScope ls(ctx, KS_KV_ATTEND, st);
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(kTcThreads), TcCfg<D>::SMEM, st, maps, a,
+                                       (const int32_t*)list, (const int32_t*)counts, part, ml, n_splits));
+    }
+    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
+}
+
+template <bool BF16>
+int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    switch (a.d) {
+        case 16: return launch_tc<16, BF16>(ctx, a, ws, st);
+        case 32: return launch_tc<32, BF16>(ctx, a, ws, st);
+        case 64: return launch_tc<64, BF16>(ctx, a, ws, st);
+        default: return launch_tc<128, BF16>(ctx, a, ws, st);
+    }
+}
+
+}  // namespace
+
+bool kv_tc_takes(const KvAttendArgs& a) {
+    return a.format == 0 && a.dtype != SENTRY_F32 && a.Tk > 0 && a.ks[2] > 0 && a.vs[2] > 0 && group_rows(a) > 32;
+}
+size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
+    const int n = tc_splits(a);
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
+    size_t bytes = 0;
+    if (n > 1) bytes += align_up(n * rows * a.d * sizeof(float), 256) + align_up(n * rows * sizeof(float2), 256);
+    // (whether the call has modality ids is not in the descriptor)
+    return bytes + align_up((size_t)a.B * a.Tk * sizeof(int32_t), 256) + align_up((size_t)a.B * sizeof(int32_t), 256) + 512;
+}
+int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    return a.dtype == SENTRY_BF16 ? launch_tc_d<true>(ctx, a, ws, st) : launch_tc_d<false>(ctx, a, ws, st);
+}
