@@ -523,12 +523,7 @@ class Sentry:
     # -- serving in 8 bits, cross attention -----------------------------------
     def quantize_rows_i8(self, X, codes=None, scales=None):
         """sentry_quantize_rows_i8.  X [..., K] -> codes int8 [..., K], scales fp32 [...] (one per row)."""
-        if codes is None:
-            codes = torch.empty(X.shape, dtype=torch.int8, device=X.device)
-        if scales is None:
-            scales = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
-        _binding.quantize_rows_i8(self, self._handle, self._ws_bytes, X, codes, scales)
-        return codes, scales
+        return _binding.quantize_rows_i8(self, self._handle, self._ws_bytes, X, codes, scales)
 
     def linear_i8(self, codes, x_scales, W, w_scales, bias=None, dtype=torch.bfloat16, Y=None):
         """sentry_linear_i8.  codes int8 [..., K], x_scales [...]; W int8 [N, K], w_scales, bias fp32 [N].  Returns Y [..., N]

@@ -458,12 +458,15 @@ int code_format(const at::Tensor& t) {
     }
 }
 
-METHOD(quantize_rows_i8) {   // X, codes, scales
-    return guarded(args, n, 3, [](Call& c) {
+METHOD(quantize_rows_i8) {   // X, codes, scales -> (codes, scales)
+    at::Tensor codes, scales;
+    PyObject* r = guarded(args, n, 3, [&](Call& c) {
         const Serving v(c, "quantize_rows_i8");
-        const at::Tensor &X = v.on_device(tensor(c.a[0])), &codes = v.on_device(tensor(c.a[1])), &scales = v.on_device(tensor(c.a[2]));
+        const at::Tensor& X = v.on_device(tensor(c.a[0]));
         if (X.dim() < 1) v.refuse("a tensor of one dimension at least");
         const int K = fits(X.size(-1)), M = K ? fits(X.numel() / K) : 0;
+        codes = v.on_device(output(c.a[1], X.sizes(), at::kChar, X));
+        scales = v.on_device(output(c.a[2], X.sizes().slice(0, X.dim() - 1), at::kFloat, X));
         if (codes.sizes() != X.sizes() || codes.scalar_type() != at::kChar || scales.scalar_type() != at::kFloat || scales.numel() != M)
             v.refuse("int8 codes of X's shape and an fp32 scale per row");
         const int type = dtype_code(X);
@@ -473,6 +476,14 @@ METHOD(quantize_rows_i8) {   // X, codes, scales
         void* st = v.stream();
         invoke("sentry_quantize_rows_i8", [&] { return sentry_quantize_rows_i8(c.ctx, M, K, type, x, cp, sp, st); });
     });
+    if (r == nullptr) return nullptr;
+    Py_DECREF(r);
+    PyObject *a = THPVariable_Wrap(codes), *b = THPVariable_Wrap(scales);
+    if (a == nullptr || b == nullptr) { Py_XDECREF(a); Py_XDECREF(b); return nullptr; }
+    PyObject* pair = PyTuple_Pack(2, a, b);
+    Py_DECREF(a);
+    Py_DECREF(b);
+    return pair;
 }
 METHOD(linear_i8) {   // codes, x_scales, W, w_scales, bias, dtype, Y
     return guarded(args, n, 7, [](Call& c) -> at::Tensor {

@@ -34,21 +34,20 @@ __device__ __noinline__ uint32_t e4m3_of(double q) {
     const double step = ldexp(1.0, max(e, -5) - 4);
     return (uint32_t)__nv_cvt_float_to_fp8((float)(rint(q / step) * step), __NV_SATFINITE, __NV_E4M3);
 }
-// Four values under scale s (0 or not a number: zero codes).  This library's e4m3 scales are powers of two, so that x / s = x * inv is
+// N values under scale s (0 or not a number: zero codes).  This library's e4m3 scales are powers of two, so that x / s = x * inv is
 // exact but for results below e4m3's smallest step, which round to 0 or to it either way; a scale of somebody else's need not be one.
-template <bool I8>
-__device__ __forceinline__ uint32_t four_codes(const float* x, float s, float inv) {
-    if (!(s >= 1.17549435e-38f)) return 0u;
-    if constexpr (I8) {
-        return pack_i8x4(round_quotient_i8(x[0], s, inv), round_quotient_i8(x[1], s, inv), round_quotient_i8(x[2], s, inv), round_quotient_i8(x[3], s, inv));
+template <bool I8, int N>
+__device__ __forceinline__ void codes_of(const float (&x)[N], float s, float inv, uint32_t (&w)[N / 4]) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = 0u;
+    if (!(s >= 1.17549435e-38f)) return;
+    if constexpr (I8) codes_i8<N>(x, s, inv, w);
+    else if (__float_as_uint(s) & 0x7fffffu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i / 4] |= e4m3_of((double)x[i] / (double)s) << (8 * (i & 3));
     } else {
-        if (__float_as_uint(s) & 0x7fffffu) {
-            uint32_t w = 0;
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) w |= e4m3_of((double)x[i] / (double)s) << (8 * i);
-            return w;
-        }
-        return e4m3x2(x[0] * inv, x[1] * inv) | (e4m3x2(x[2] * inv, x[3] * inv) << 16);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) w[i] = e4m3x2(x[4 * i] * inv, x[4 * i + 1] * inv) | (e4m3x2(x[4 * i + 2] * inv, x[4 * i + 3] * inv) << 16);
     }
 }
 // A stored code under a larger scale: code * old / now to the nearest code.  (Doubles hold the product exactly, and the quotient to
@@ -66,7 +65,7 @@ __device__ uint8_t again(uint8_t c, float old, float now) {
 }
 
 template <typename T, bool I8>
-__global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const AppendArgs a, int page_blocks) {
+__global__ void __launch_bounds__(kAppThreads, 2) cache_append_kernel(const AppendArgs a, int page_blocks) {
     constexpr int N = Vec16<T>::N;
     __shared__ int s_token[128];
     __shared__ int s_count[kAppThreads / 32];
@@ -127,49 +126,37 @@ __global__ void __launch_bounds__(kAppThreads) cache_append_kernel(const AppendA
     }
     __syncthreads();
     const int slot0 = start - at * page;
-    const int per_row = d / N, pieces = n * per_row;       // 16-byte pieces of a row, and of all
+    const int shift = 31 - __clz(d / N), per_row = 1 << shift, pieces = n << shift;    // 16-byte pieces of a row, and of all
     for (int unit = warp; unit < 2 * Hk; unit += kAppThreads / 32) {
         const bool is_v = unit >= Hk;
         const int h = is_v ? unit - Hk : unit;
-        const long long* st = is_v ? a.vs : a.ks;
-        const T* src = (const T*)(is_v ? a.V : a.K) + b * st[0] + h * st[1];
+        const long long step = is_v ? a.vs[2] : a.ks[2];
+        const T* src = is_v ? (const T*)a.V + b * a.vs[0] + h * a.vs[1] : (const T*)a.K + b * a.ks[0] + h * a.ks[1];
         uint8_t* codes = (uint8_t*)(is_v ? a.c.v : a.c.k) + ((size_t)id * Hk + h) * page * d;
         float* scale = (is_v ? a.c.v_scales : a.c.k_scales) + (size_t)id * Hk + h;
         const float old = slot0 > 0 ? *scale : 0.0f;
-        auto piece = [&](int p) { return *reinterpret_cast<const uint4*>(src + s_token[p / per_row] * st[2] + (p % per_row) * N); };
+        auto piece = [&](int p) { return *reinterpret_cast<const uint4*>(src + s_token[p >> shift] * step + (p & (per_row - 1)) * N); };
         uint4 held[kHold];
+        AbsMax<T> top;
 #pragma unroll
         for (int i = 0; i < kHold; ++i) held[i] = i * 32 + lane < pieces ? piece(i * 32 + lane) : make_uint4(0, 0, 0, 0);
-        float top = 0.0f;
-        bool bad = false;
-        auto look = [&](const uint4& v) {
-            float f[N];
-            Vec16<T>::get(v, f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float m = fabsf(f[j]);
-                bad = bad || !(m <= 3.4028234e38f);
-                top = fmaxf(top, m);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < kHold; ++i) look(held[i]);
-        for (int p = kHold * 32 + lane; p < pieces; p += 32) look(piece(p));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        bad = __any_sync(0xffffffffu, bad) || isnan(old);
-        const float need = page_scale<I8>(top);
-        const float now = bad ? nan_f32() : fmaxf(need, old);
+        for (int i = 0; i < kHold; ++i) top.add(held[i]);
+        for (int p = kHold * 32 + lane; p < pieces; p += 32) top.add(piece(p));
+        const float most = magnitude<T>(__reduce_max_sync(0xffffffffu, top.bits()));
+        const float now = isnan(most) || isnan(old) ? nan_f32() : fmaxf(page_scale<I8>(most), old);
         const float inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
         // older codes of the page under its new scale
         if (slot0 > 0 && !(now == old))
             for (int i = lane; i < slot0 * d; i += 32) codes[i] = again<I8>(codes[i], old, now);
+        uint8_t* dst = codes + (size_t)slot0 * d;
         auto store = [&](const uint4& v, int p) {
             float f[N];
+            uint32_t w[N / 4];
             Vec16<T>::get(v, f);
-            uint8_t* dst = codes + (size_t)(slot0 + p / per_row) * d + (p % per_row) * N;
-            if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(four_codes<I8>(f, now, inv), four_codes<I8>(f + 4, now, inv));
-            else *reinterpret_cast<uint32_t*>(dst) = four_codes<I8>(f, now, inv);
+            codes_of<I8, N>(f, now, inv, w);
+            if constexpr (N == 8) *reinterpret_cast<uint2*>(dst + (size_t)p * 8) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(dst + (size_t)p * 4) = w[0];
         };
 #pragma unroll
         for (int i = 0; i < kHold; ++i)

@@ -3,36 +3,61 @@
 
 namespace {
 
-// Joins the parts of a split axis: a warp per row.
+// A block per row: its warps take every fourth part, with the loads of several on the way, and meet in shared memory.  (A warp per row, part
+// after part: 37 us for 16 rows of 128 parts.)
 template <bool BF16>
 __global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int n_splits) {
-    const int lane = threadIdx.x & 31;
-    const size_t rows = (size_t)a.B * a.k_h * a.Tq, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    __shared__ float s_weight[128], s_acc[4][128];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const size_t rows = (size_t)a.B * a.k_h * a.Tq, row = blockIdx.x;
     grid_dependency_wait();
-    if (row >= rows) return;
     const int j = (int)(row / a.Tq % a.k_h), b = (int)(row / a.Tq / a.k_h);
     if (kv_head(a, b, j) < 0) return;         // (its zero rows are written)
-    float top = -INFINITY;
-    for (int s = lane; s < n_splits; s += 32) top = fmaxf(top, ml[s * rows + row].x);
+    // every warp by itself: the maximum, the total, and the weights of all parts (128 at most)
+    float2 x[4];
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int s = i * 32 + lane;
+        x[i] = s < n_splits ? ml[s * rows + row] : make_float2(-INFINITY, 0.0f);
+        top = fmaxf(top, x[i].x);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float ref = top == -INFINITY ? 0.0f : top;
-    float acc[4] = {}, sum = 0.0f;
-    const int cols = a.d / 32 ? a.d / 32 : 1, c0 = lane * cols;
-    for (int s = 0; s < n_splits; ++s) {
-        const float2 x = ml[s * rows + row];
-        const float f = exp2_fast(x.x - ref);
-        sum += x.y * f;
-        if (x.x == -INFINITY && x.y == 0.0f) continue;    // (nothing seen there)
-        if (c0 < a.d)
-            for (int c = 0; c < cols; ++c) acc[c] += part[(s * rows + row) * a.d + c0 + c] * f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float f = exp2_fast(x[i].x - ref);
+        total += x[i].y * f;
+        // (a part that saw nothing was not written)
+        if (warp == 0 && i * 32 + lane < n_splits) s_weight[i * 32 + lane] = x[i].x == -INFINITY && x[i].y == 0.0f ? -1.0f : f;
     }
-    if (c0 < a.d)
-        for (int c = 0; c < cols; ++c) {
-            const float v = sum == 0.0f ? 0.0f : acc[c] / sum;
-            if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(a.O)[row * a.d + c0 + c] = __float2bfloat16_rn(v);
-            else reinterpret_cast<__half*>(a.O)[row * a.d + c0 + c] = __float2half_rn(v);
-        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    __syncthreads();
+    // columns: four floats a lane, 16 to 128 of them; the lanes that are left over take further parts
+    const int lanes = a.d / 4, sub = lane / lanes, subs = 32 / lanes, c = lane % lanes;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+    for (int s = warp * subs + sub; s < n_splits; s += 4 * subs) {
+        const float f = s_weight[s];
+        if (f < 0.0f) continue;
+        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + row) * a.d + c * 4);
+        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+    }
+    for (int o = lanes; o < 32; o <<= 1) {
+        acc.x += __shfl_xor_sync(0xffffffffu, acc.x, o);
+        acc.y += __shfl_xor_sync(0xffffffffu, acc.y, o);
+        acc.z += __shfl_xor_sync(0xffffffffu, acc.z, o);
+        acc.w += __shfl_xor_sync(0xffffffffu, acc.w, o);
+    }
+    if (sub == 0) *reinterpret_cast<float4*>(&s_acc[warp][c * 4]) = acc;
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.d; e += 128) {
+        const float v = total == 0.0f ? 0.0f : (s_acc[0][e] + s_acc[1][e] + s_acc[2][e] + s_acc[3][e]) / total;
+        if constexpr (BF16) reinterpret_cast<__nv_bfloat16*>(a.O)[row * a.d + e] = __float2bfloat16_rn(v);
+        else reinterpret_cast<__half*>(a.O)[row * a.d + e] = __float2half_rn(v);
+    }
 }
 
 }  // namespace
@@ -41,6 +66,6 @@ int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part,
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     LaunchScope ls(ctx, KS_KV_COMBINE, st);
     auto k = a.dtype == SENTRY_BF16 ? kv_combine_kernel<true> : kv_combine_kernel<false>;
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a, part, ml, n_splits));
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)rows), dim3(128), 0, st, a, part, ml, n_splits));
     return SENTRY_OK;
 }

@@ -514,7 +514,8 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
     auto k = kv_rows_kernel<KV, D, BF16>;
-    SENTRY_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    static std::atomic<unsigned long long> allowed{0};
+    SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
         SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)(row_tiles < 64 ? row_tiles : 64)), dim3(kWarps * 32), C::SMEM, st, a,

@@ -437,7 +437,8 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
         SENTRY_CUDA_TRY(launch_chained(kv_plan_kernel, dim3((unsigned)a.B), dim3(1024), 0, st, a, list, counts));
     }
     auto k = kv_tc_kernel<D, BF16>;
-    SENTRY_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<D>::SMEM));
+    static std::atomic<unsigned long long> allowed{0};
+    SENTRY_CUDA_TRY(allow_smem(k, TcCfg<D>::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
         SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(kTcThreads), TcCfg<D>::SMEM, st, maps, a,

@@ -5,21 +5,22 @@
 //   linear_i8_tc_kernel     tcgen05 kind::i8, operands by TMA, accumulators in tensor memory
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "serving.cuh"
 #include "tc_common.cuh"
 
 namespace {
 
 // ------------------------------------------------------------------------------------------------ quantise rows
-// WARPS warps share a row (1: eight rows a block; 8: one row a block).  Up to HELD pieces of 16 bytes a lane stay in registers; what a
-// longer row has beyond them is read a second time.
-constexpr int kHeld = 8;
-
-template <typename T, int WARPS>
+// WARPS warps share a row (1: eight rows a block; 8: one row a block).  Up to HELD pieces of 16 bytes a lane stay in registers between the
+// two steps; what a longer row has beyond them is read a second time.  Bound by the bytes, as long as a value costs few instructions:
+// the maximum runs on pairs of magnitude bits, and the quotient is rounded by an addition unless it lies next to a half (codes_i8).
+template <typename T, int WARPS, int HELD>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ X, int8_t* __restrict__ codes, float* __restrict__ scales,
                                                             int M, int K) {
     constexpr int N = Vec16<T>::N, LANES = 32 * WARPS;
-    __shared__ float s_top[8];
+    __shared__ uint32_t s_top[8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long row = WARPS == 1 ? (long long)blockIdx.x * 8 + warp : blockIdx.x;
     const int at = WARPS == 1 ? lane : (int)threadIdx.x;
@@ -28,73 +29,53 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
     if (row >= M) return;                 // (whole warps, and no block-wide step follows where WARPS is 1)
     const uint4* src = reinterpret_cast<const uint4*>(X + row * K);
     const int pieces = K / N;
-    uint4 held[kHeld];
-    float top = 0.0f;
-    bool bad = false;
-    auto look = [&](const uint4& v) {
-        float f[N];
-        Vec16<T>::get(v, f);
+    uint4 held[HELD];
+    AbsMax<T> top;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float a = fabsf(f[i]);
-            bad = bad || !(a <= 3.4028234e38f);
-            top = fmaxf(top, a);
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
         const int p = at + i * LANES;
         held[i] = p < pieces ? src[p] : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) look(held[i]);
-    for (int p = at + kHeld * LANES; p < pieces; p += LANES) look(src[p]);
-    if (bad) top = __int_as_float(0x7fc00000);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float other = __shfl_xor_sync(0xffffffffu, top, o);
-        top = (isnan(top) || isnan(other)) ? __int_as_float(0x7fc00000) : fmaxf(top, other);
-    }
+    for (int i = 0; i < HELD; ++i) top.add(held[i]);
+    for (int p = at + HELD * LANES; p < pieces; p += LANES) top.add(src[p]);
+    uint32_t bits = __reduce_max_sync(0xffffffffu, top.bits());
     if (WARPS > 1) {
-        if (lane == 0) s_top[warp] = top;
+        if (lane == 0) s_top[warp] = bits;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) top = (isnan(top) || isnan(s_top[w])) ? __int_as_float(0x7fc00000) : fmaxf(top, s_top[w]);
+        for (int w = 0; w < WARPS; ++w) bits = max(bits, s_top[w]);
     }
-    const bool nan = isnan(top);
-    const float s = nan ? top : scale_i8(top);
+    const float most = magnitude<T>(bits);
+    const float s = isnan(most) ? most : scale_i8(most);
     const float inv = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
     if (at == 0) scales[row] = s;
     int8_t* dst = codes + row * K;
     auto put = [&](const uint4& v, int p) {
         float f[N];
+        uint32_t w[N / 4] = {};
         Vec16<T>::get(v, f);
-        uint32_t w[N / 4];
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            int c[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) c[j] = s > 0.0f ? round_quotient_i8(f[4 * i + j], s, inv) : 0;
-            w[i] = pack_i8x4(c[0], c[1], c[2], c[3]);
-        }
+        if (s > 0.0f) codes_i8<N>(f, s, inv, w);
         if constexpr (N == 8) *reinterpret_cast<uint2*>(dst + (size_t)p * 8) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(dst + (size_t)p * 4) = w[0];
     };
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
         const int p = at + i * LANES;
         if (p < pieces) put(held[i], p);
     }
-    for (int p = at + kHeld * LANES; p < pieces; p += LANES) put(src[p], p);
+    for (int p = at + HELD * LANES; p < pieces; p += LANES) put(src[p], p);
 }
 
 template <typename T>
 int launch_quantize(sentry_ctx* ctx, int M, int K, const void* X, int8_t* codes, float* scales, cudaStream_t st) {
     LaunchScope ls(ctx, KS_QUANTIZE, st);
+    const int pieces = K / Vec16<T>::N;
     // a warp per row where that fills the GPU and the row fits its registers
-    const bool one = (long long)M >= 8LL * ctx->sm_count && K / Vec16<T>::N <= 32 * kHeld;
-    if (one) SENTRY_CUDA_TRY(launch_chained(quantize_rows_kernel<T, 1>, dim3((unsigned)((M + 7) / 8)), dim3(256), 0, st, (const T*)X, codes, scales, M, K));
-    else SENTRY_CUDA_TRY(launch_chained(quantize_rows_kernel<T, 8>, dim3((unsigned)M), dim3(256), 0, st, (const T*)X, codes, scales, M, K));
+    const bool one = (long long)M >= 8LL * ctx->sm_count && pieces <= 32 * 8;
+    auto k = one ? (pieces <= 64 ? quantize_rows_kernel<T, 1, 2> : pieces <= 128 ? quantize_rows_kernel<T, 1, 4> : quantize_rows_kernel<T, 1, 8>)
+                 : (pieces <= 256 ? quantize_rows_kernel<T, 8, 1> : quantize_rows_kernel<T, 8, 8>);
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(one ? (M + 7) / 8 : M)), dim3(256), 0, st, (const T*)X, codes, scales, M, K));
     return SENTRY_OK;
 }
 
@@ -168,28 +149,39 @@ int launch_few(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
 }
 
 // ------------------------------------------------------------------------------------------------ tcgen05
-// D[tmem] (+)= A[smem] * B[smem], s8 x s8 -> s32, 32 bytes of K a step; issued by one thread.
+// D[tmem] (+)= A[smem] * B[smem], s8 x s8 -> s32, 32 bytes of K a step; issued by one thread.  P: 2 for a pair of CTAs.
+template <int P>
 __device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-        :
-        : "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
+    if constexpr (P == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc),
+                     "l"(b_desc), "r"(idesc), "r"(accumulate)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc),
+                     "l"(b_desc), "r"(idesc), "r"(accumulate)
+                     : "memory");
 }
 // accumulator s32 (2), both operands s8 (1), K-major
 __host__ __device__ constexpr uint32_t umma_idesc_i8(int M, int N) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-constexpr int kLinBM = 128, kLinBN = 256, kLinStages = 4, kLinThreads = 256;
-constexpr int kLinStageBytes = (kLinBM + kLinBN) * 128;
-constexpr int kLinStore = 4 * 32 * 128;   // an epilogue warp's 32 rows of 128 bytes
-constexpr int kLinSmem = kLinStages * kLinStageBytes + kLinStore + 1024 + 1024;
+// A tile: 128 P tokens x BN channels, K in steps of 128 bytes; a pair's CTAs have 128 tokens and half of the channels' weights each, so that
+// a tile costs the L2 and shared memory two thirds of what two single CTAs' would.  Two accumulators in tensor memory: the eight
+// epilogue warps scale and store one while the other is summed.
+constexpr int kLinThreads = 384, kLinEpiWarp0 = 4, kLinEpiWarps = 8;
 
+template <int P, int BN>
+struct LinCfg {
+    static constexpr int B_ROWS = BN / P;
+    static constexpr int STAGE = (128 + B_ROWS) * 128;
+    static constexpr int STAGES = 163840 / STAGE > 8 ? 8 : 163840 / STAGE;
+    static constexpr int TMEM = BN <= 64 ? 128 : BN <= 128 ? 256 : 512;
+    static constexpr int EPI = 4096 + (BN < 128 ? 128 : BN) * 4;                // a warp's 32 rows of 128 bytes; scales and biases of its half of the columns
+    static constexpr int SMEM = STAGES * STAGE + kLinEpiWarps * EPI + 1024;
+};
 struct LinMisc {
-    uint64_t full[kLinStages], empty[kLinStages], acc_full[2], acc_empty[2];
+    uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -206,24 +198,26 @@ bool make_map_i8(CUtensorMap* tm, const void* ptr, uint64_t rows, uint64_t K, ui
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T>
+template <typename T, int P, int BN>
 __global__ void __launch_bounds__(kLinThreads, 1)
 linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const float* __restrict__ xs,
                     const float* __restrict__ ws, const float* __restrict__ bias, T* __restrict__ Y, int M, int K, int N, unsigned int* status) {
+    using C = LinCfg<P, BN>;
     extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw_addr = ptx::smem_u32(smem_raw);
-    const uint32_t base = (raw_addr + 1023u) & ~1023u;
-    LinMisc* misc = reinterpret_cast<LinMisc*>(smem_raw + (base - raw_addr) + kLinStages * kLinStageBytes + kLinStore);
+    __shared__ LinMisc misc_s;
+    LinMisc* misc = &misc_s;
+    const uint32_t raw_addr = ptx::smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;
     volatile int* abort_flag = &misc->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = P == 2 ? (int)ptx::cluster_rank() : 0;      // CTA 0 of a pair issues the UMMAs of both
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kLinStages; ++s) {
+        for (int s = 0; s < C::STAGES; ++s) {
             ptx::mbar_init(ptx::smem_u32(&misc->full[s]), 1);
             ptx::mbar_init(ptx::smem_u32(&misc->empty[s]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(ptx::smem_u32(&misc->acc_full[s]), 1);
-            ptx::mbar_init(ptx::smem_u32(&misc->acc_empty[s]), 4);
+            ptx::mbar_init(ptx::smem_u32(&misc->acc_empty[s]), P * kLinEpiWarps);
         }
         misc->abort_flag = 0;
         ptx::fence_barrier_init();
@@ -231,144 +225,203 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
         ptx::prefetch_tensormap(&tm_w);
     }
     if (warp == 0) {
-        ptx::tmem_alloc(ptx::smem_u32(&misc->tmem_base), 512);
-        ptx::tmem_relinquish();
+        if constexpr (P == 2) { ptx::tmem_alloc_pair(ptx::smem_u32(&misc->tmem_base), C::TMEM); ptx::tmem_relinquish_pair(); }
+        else { ptx::tmem_alloc(ptx::smem_u32(&misc->tmem_base), C::TMEM); ptx::tmem_relinquish(); }
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
+    if constexpr (P == 2) ptx::cluster_sync();                   // the other CTA's barriers are initialised
     ptx::tc_fence_after_sync();
     const uint32_t tmem = misc->tmem_base;
     grid_dependency_wait();
-    const int n_tiles = (N + kLinBN - 1) / kLinBN, m_tiles = (M + kLinBM - 1) / kLinBM;
-    const long long tiles = (long long)n_tiles * m_tiles;
+    const int n_tiles = (N + BN - 1) / BN;
+    const long long tiles = (long long)n_tiles * ((M + 128 * P - 1) / (128 * P));
+    const long long tile0 = blockIdx.x / P, tile_step = gridDim.x / P;
     const int KB = (K + 127) / 128;
 
     if (warp == 0) {
         bool ok = true;
         uint32_t it = 0;
-        for (long long tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-            const int m0 = (int)(tile / n_tiles) * kLinBM, n0 = (int)(tile % n_tiles) * kLinBN;
+        for (long long tile = tile0; tile < tiles && ok; tile += tile_step) {
+            const int m0 = (int)(tile / n_tiles) * 128 * P + rank * 128, n0 = (int)(tile % n_tiles) * BN + rank * C::B_ROWS;
             for (int kb = 0; kb < KB && ok; ++kb, ++it) {
-                const uint32_t s = it % kLinStages, use = it / kLinStages;
+                const uint32_t s = it % C::STAGES, use = it / C::STAGES;
                 ok = warp_wait(&misc->empty[s], (use & 1) ^ 1, abort_flag);
                 if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t bar = ptx::smem_u32(&misc->full[s]), dst = base + s * kLinStageBytes;
-                    ptx::mbar_arrive_expect_tx(bar, kLinStageBytes);
-                    ptx::tma_load_2d(dst, &tm_x, kb * 128, m0, bar);
-                    ptx::tma_load_2d(dst + kLinBM * 128, &tm_w, kb * 128, n0, bar);
+                    const uint32_t bar = ptx::smem_u32(&misc->full[s]), dst = base + s * C::STAGE;
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(bar, P * C::STAGE);
+                    if constexpr (P == 2) {
+                        const uint32_t bar0 = ptx::cluster_addr(bar, 0);
+                        ptx::tma_load_2d_pair(dst, &tm_x, kb * 128, m0, bar0);
+                        ptx::tma_load_2d_pair(dst + 128 * 128, &tm_w, kb * 128, n0, bar0);
+                    } else {
+                        ptx::tma_load_2d(dst, &tm_x, kb * 128, m0, bar);
+                        ptx::tma_load_2d(dst + 128 * 128, &tm_w, kb * 128, n0, bar);
+                    }
                 }
                 __syncwarp();
             }
         }
-    } else if (warp == 1) {
-        const uint32_t idesc = umma_idesc_i8(kLinBM, kLinBN);
+    } else if (warp == 1 && rank == 0) {
+        constexpr uint32_t idesc = umma_idesc_i8(128 * P, BN);
+        // (in a pair, the other CTA's copies and threads arrive on these barriers too)
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+            const bool got = warp_wait(bar, parity, abort_flag);
+            if constexpr (P == 2) { if (got) (void)ptx::mbar_try_wait_cluster(ptx::smem_u32(bar), parity); }   // acquired at cluster scope too
+            return got;
+        };
         bool ok = true;
         uint32_t it = 0, n = 0;
-        for (long long tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++n) {
-            const uint32_t buf = n & 1, acc = tmem + buf * kLinBN;
-            ok = warp_wait(&misc->acc_empty[buf], ((n >> 1) & 1) ^ 1, abort_flag);
+        for (long long tile = tile0; tile < tiles && ok; tile += tile_step, ++n) {
+            const uint32_t buf = n & 1, acc = tmem + buf * BN;
+            ok = wait(&misc->acc_empty[buf], ((n >> 1) & 1) ^ 1);
+            if (!ok) break;
             ptx::tc_fence_after_sync();
             for (int kb = 0; kb < KB && ok; ++kb, ++it) {
-                const uint32_t s = it % kLinStages, use = it / kLinStages;
-                ok = warp_wait(&misc->full[s], use & 1, abort_flag);
+                const uint32_t s = it % C::STAGES, use = it / C::STAGES;
+                ok = wait(&misc->full[s], use & 1);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
                 if (elect_one()) {
-                    const uint32_t a = base + s * kLinStageBytes, b = a + kLinBM * 128;
+                    const uint32_t a = base + s * C::STAGE, b = a + 128 * 128;
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        umma_i8(acc, ptx::umma_smem_desc_sw128(a + ks * 32), ptx::umma_smem_desc_sw128(b + ks * 32), idesc, (kb > 0 || ks > 0) ? 1u : 0u);
-                    ptx::umma_commit(ptx::smem_u32(&misc->empty[s]));
-                    if (kb == KB - 1) ptx::umma_commit(ptx::smem_u32(&misc->acc_full[buf]));
+                        umma_i8<P>(acc, ptx::umma_smem_desc_sw128(a + ks * 32), ptx::umma_smem_desc_sw128(b + ks * 32), idesc, (kb > 0 || ks > 0) ? 1u : 0u);
+                    if constexpr (P == 2) ptx::umma_commit_pair(ptx::smem_u32(&misc->empty[s]));
+                    else ptx::umma_commit(ptx::smem_u32(&misc->empty[s]));
+                    if (kb == KB - 1) {
+                        if constexpr (P == 2) ptx::umma_commit_pair(ptx::smem_u32(&misc->acc_full[buf]));
+                        else ptx::umma_commit(ptx::smem_u32(&misc->acc_full[buf]));
+                    }
                 }
                 __syncwarp();
             }
         }
-    } else if (warp >= 4) {
-        // rows of this warp's quarter; 128 bytes of every row at a time through shared memory, so that stores write whole lines
-        constexpr int COLS = 128 / (int)sizeof(T);    // 64 or 32 columns
-        const int quarter = warp & 3;
-        const uint32_t stg = base + kLinStages * kLinStageBytes + quarter * 4096;
+    } else if (warp >= kLinEpiWarp0) {
+        // Rows of this warp's quarter and every other 128 bytes of columns, through shared memory, so that stores write whole lines.
+        constexpr int COLS = 128 / (int)sizeof(T), STEPS = BN / (2 * COLS) > 0 ? BN / (2 * COLS) : 1, PER = 16 / (int)sizeof(T);
+        const int quarter = warp & 3, half = (warp - kLinEpiWarp0) >> 2;
+        const uint32_t own = C::STAGES * C::STAGE + (base - raw_addr) + (warp - kLinEpiWarp0) * C::EPI;
+        const uint32_t stg = raw_addr + own;
+        float* s_scale = reinterpret_cast<float*>(smem_raw + own + 4096);     // [STEPS * COLS] scales, then biases
+        float* s_bias = s_scale + STEPS * COLS;
         bool ok = true;
         uint32_t n = 0;
-        const bool whole = N % (16 / (int)sizeof(T)) == 0;    // rows of Y start on 16 bytes
-        for (long long tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++n) {
-            const uint32_t buf = n & 1, acc = tmem + buf * kLinBN + ((uint32_t)(quarter * 32) << 16);
-            const int m0 = (int)(tile / n_tiles) * kLinBM + quarter * 32, n0 = (int)(tile % n_tiles) * kLinBN;
+        const bool whole = N % PER == 0;                                      // rows of Y start on 16 bytes
+        for (long long tile = tile0; tile < tiles && ok; tile += tile_step, ++n) {
+            const uint32_t buf = n & 1, acc = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
+            const int m0 = (int)(tile / n_tiles) * 128 * P + rank * 128 + quarter * 32, n0 = (int)(tile % n_tiles) * BN;
             const float sx = m0 + lane < M ? xs[m0 + lane] : 0.0f;
+#pragma unroll
+            for (int e = lane; e < STEPS * COLS; e += 32) {
+                const int col = n0 + (e / COLS * 2 + half) * COLS + e % COLS;
+                s_scale[e] = col < N ? ws[col] : 0.0f;
+                s_bias[e] = bias != nullptr && col < N ? bias[col] : 0.0f;
+            }
+            __syncwarp();
             ok = warp_wait(&misc->acc_full[buf], (n >> 1) & 1, abort_flag);
             if (!ok) break;
             ptx::tc_fence_after_sync();
-            for (int c0 = 0; c0 < kLinBN && n0 + c0 < N; c0 += COLS) {
-                uint32_t w[32];
+#pragma unroll 1
+            for (int step = 0; step < STEPS; ++step) {
+                const int c0 = (step * 2 + half) * COLS;
+                if (c0 >= BN || n0 + c0 >= N) break;
+                uint32_t r[COLS / 32][32];
 #pragma unroll
-                for (int h = 0; h < COLS / 32; ++h) {
-                    uint32_t r[32];
-                    ptx::tmem_ld_32x32(acc + c0 + h * 32, r);
-                    ptx::tmem_ld_wait();
+                for (int h = 0; h < COLS / 32; ++h) ptx::tmem_ld_32x32(acc + c0 + h * 32, r[h]);
+                ptx::tmem_ld_wait();
+                const float4* sc4 = reinterpret_cast<const float4*>(s_scale + step * COLS);
+                const float4* bi4 = reinterpret_cast<const float4*>(s_bias + step * COLS);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int col = n0 + c0 + h * 32 + i;
-                        const bool in = col < N;
-                        float y = (float)(int32_t)r[i] * sx * (in ? __ldg(ws + col) : 0.0f);
-                        if (bias != nullptr && in) y += __ldg(bias + col);
-                        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(y);
-                        else {
-                            const T v = from_f32<T>(y);
-                            const uint32_t bits = *reinterpret_cast<const unsigned short*>(&v);
-                            if (i & 1) w[h * 16 + i / 2] |= bits << 16;
-                            else w[h * 16 + i / 2] = bits;
+                for (int i = 0; i < COLS; i += PER) {
+                    float y[PER];
+#pragma unroll
+                    for (int x = 0; x < PER; x += 4) {
+                        const float4 f = sc4[(i + x) / 4], c = bi4[(i + x) / 4];
+                        const uint32_t* q = &r[(i + x) / 32][(i + x) % 32];
+                        y[x] = fmaf((float)(int32_t)q[0] * sx, f.x, c.x);
+                        y[x + 1] = fmaf((float)(int32_t)q[1] * sx, f.y, c.y);
+                        y[x + 2] = fmaf((float)(int32_t)q[2] * sx, f.z, c.z);
+                        y[x + 3] = fmaf((float)(int32_t)q[3] * sx, f.w, c.w);
+                    }
+                    uint32_t w[4];
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) w[x] = __float_as_uint(y[x]);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            if constexpr (std::is_same_v<T, __half>) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[x]) : "f"(y[2 * x + 1]), "f"(y[2 * x]));
+                            else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[x]) : "f"(y[2 * x + 1]), "f"(y[2 * x]));
                         }
                     }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stg + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(w[4 * i]),
-                                 "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stg + lane * 128 + (((i / PER) ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                                 "r"(w[3])
                                  : "memory");
+                }
                 __syncwarp();
+                if (whole) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = i * 4 + (lane >> 3), ch = lane & 7, col = n0 + c0 + ch * (16 / (int)sizeof(T));
-                    uint4 v;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stg + row * 128 + ((ch ^ (row & 7)) << 4)));
-                    if (m0 + row >= M) continue;
-                    T* dst = Y + (size_t)(m0 + row) * N + col;
-                    if (whole) {
-                        if (col < N) *reinterpret_cast<uint4*>(dst) = v;
-                    } else {
-                        const T* e = reinterpret_cast<const T*>(&v);
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = i * 4 + (lane >> 3), ch = lane & 7, col = n0 + c0 + ch * PER;
+                        uint4 v;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stg + row * 128 + ((ch ^ (row & 7)) << 4)));
+                        if (m0 + row < M && col < N) *reinterpret_cast<uint4*>(Y + (size_t)(m0 + row) * N + col) = v;
+                    }
+                } else {
+                    // rows that start anywhere: neighbouring lanes store neighbouring elements
+                    const T* line = reinterpret_cast<const T*>(smem_raw + own);
+#pragma unroll 4
+                    for (int row = 0; row < 32 && m0 + row < M; ++row) {
 #pragma unroll
-                        for (int j = 0; j < 16 / (int)sizeof(T); ++j)
-                            if (col + j < N) dst[j] = e[j];
+                        for (int h = 0; h < COLS / 32; ++h) {
+                            const int e = h * 32 + lane, col = n0 + c0 + e;
+                            const T v = line[row * COLS + ((e / PER) ^ (row & 7)) * PER + e % PER];
+                            if (col < N) Y[(size_t)(m0 + row) * N + col] = v;
+                        }
                     }
                 }
                 __syncwarp();
             }
             ptx::tc_fence_before_sync();
-            warp_arrive(&misc->acc_empty[buf]);
+            __syncwarp();
+            if (lane == 0) {
+                const uint32_t bar = ptx::smem_u32(&misc->acc_empty[buf]);
+                if constexpr (P == 2) ptx::mbar_arrive_cluster(ptx::cluster_addr(bar, 0));
+                else ptx::mbar_arrive(bar);
+            }
         }
     }
-    tc_cta_teardown(abort_flag, status, tmem, 512);
+    if constexpr (P == 2) {
+        __syncwarp();
+        ptx::cluster_sync();                    // the pair's UMMAs read both CTAs' shared memory, its barriers hear from both
+    }
+    tc_cta_teardown<P>(abort_flag, status, tmem, C::TMEM);
 }
 
-template <typename T>
+template <typename T, int P, int BN>
 int launch_tc(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
+    using C = LinCfg<P, BN>;
     CUtensorMap mx, mw;
-    if (!make_map_i8(&mx, a.X, a.d.M, a.d.K, kLinBM) || !make_map_i8(&mw, a.W, a.d.N, a.d.K, kLinBN)) return SENTRY_ERR_CUDA;
-    const long long tiles = (long long)((a.d.M + kLinBM - 1) / kLinBM) * ((a.d.N + kLinBN - 1) / kLinBN);
-    auto k = linear_i8_tc_kernel<T>;
-    SENTRY_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem));
+    if (!make_map_i8(&mx, a.X, a.d.M, a.d.K, 128) || !make_map_i8(&mw, a.W, a.d.N, a.d.K, C::B_ROWS)) return SENTRY_ERR_CUDA;
+    const long long tiles = (long long)((a.d.M + 128 * P - 1) / (128 * P)) * ((a.d.N + BN - 1) / BN), most = ctx->sm_count / P;
+    auto k = linear_i8_tc_kernel<T, P, BN>;
+    static std::atomic<unsigned long long> allowed{0};
+    SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     LaunchScope ls(ctx, KS_LINEAR, st);
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count)), dim3(kLinThreads), kLinSmem, st, mx, mw, a.xs, a.ws,
-                                   a.bias, (T*)a.Y, a.d.M, a.d.K, a.d.N, a.status));
+    SENTRY_CUDA_TRY(launch_chained_clusters(P, k, dim3((unsigned)((tiles < most ? tiles : most) * P)), dim3(kLinThreads), C::SMEM, st, mx, mw, a.xs, a.ws, a.bias,
+                                            (T*)a.Y, a.d.M, a.d.K, a.d.N, a.status));
     return SENTRY_OK;
 }
 
 template <typename T>
 int launch_linear(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
-    return a.d.M <= 64 ? launch_few<T>(ctx, a, st) : launch_tc<T>(ctx, a, st);
+    if (a.d.M <= 64) return launch_few<T>(ctx, a, st);
+    // pairs where their tiles fill the GPU; else narrower tiles, so that more SMs have one
+    auto tiles = [&](long long m, long long n) { return ((a.d.M + m - 1) / m) * ((a.d.N + n - 1) / n); };
+    if (2 * tiles(256, 256) >= ctx->sm_count) return launch_tc<T, 2, 256>(ctx, a, st);
+    return 2 * tiles(128, 128) >= ctx->sm_count ? launch_tc<T, 1, 128>(ctx, a, st) : launch_tc<T, 1, 64>(ctx, a, st);
 }
 
 }  // namespace

@@ -1,7 +1,19 @@
 // Declarations shared by the serving operators (8-bit linear layer, cross attention, 8-bit cache): argument structs, launchers and
 // the integer rounding that two of them use.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
+
+// Lets a kernel have `bytes` of dynamic shared memory; once per device (`done` is the caller's, one per kernel).
+template <typename F>
+static inline cudaError_t allow_smem(F* kernel, int bytes, int device, std::atomic<unsigned long long>& done) {
+    const unsigned long long bit = device < 64 ? 1ull << device : 0ull;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 constexpr int kServeMaxHeads = 256;
 
@@ -62,8 +74,33 @@ __device__ __forceinline__ int round_quotient_i8(float x, float s, float inv) {
     else if (e2 < -s || (e2 == -s && odd)) r -= 1.0f;
     return (int)fminf(fmaxf(r, -127.0f), 127.0f);
 }
-__device__ __forceinline__ uint32_t pack_i8x4(int a, int b, int c, int d) {
-    return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)(d & 255) << 24);
+// Eight values over s (positive): codes as two words.  x * inv is within 127 * 2^-23 of the quotient, so that its nearest integer is the
+// quotient's unless it lies that near to a half; adding 1.5 * 2^23 rounds and leaves the integer in the low bits.
+__device__ __forceinline__ uint32_t pack_low_bytes(float a, float b, float c, float d) {
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
+template <int N>
+__device__ __forceinline__ void codes_i8(const float (&x)[N], float s, float inv, uint32_t (&w)[N / 4]) {
+    constexpr float kMagic = 12582912.0f;
+    float y[N], far = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        y[i] = fmaf(x[i], inv, kMagic);
+        far = fmaxf(far, fabsf(fmaf(x[i], inv, kMagic - y[i])));
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = pack_low_bytes(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+    if (far > 0.4999f) {
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+            float v = x[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) v = j == i ? x[j] : v;       // (no indexed registers)
+            const uint32_t c = (uint32_t)(round_quotient_i8(v, s, inv) & 255) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
+#pragma unroll
+            for (int j = 0; j < N / 4; ++j) w[j] = j == i / 4 ? (w[j] & keep) | c : w[j];
+        }
+    }
 }
 // (the product with 1/127 rounded to fp32, not the quotient: what the header defines)
 __device__ __forceinline__ float scale_i8(float top) { return top > 0.0f ? fmaxf(__fmul_rn(top, 1.0f / 127.0f), 1.17549435e-38f) : 0.0f; }
@@ -95,4 +132,26 @@ template <> struct Vec16<__half> {
         }
     }
 };
+
+// The largest magnitude of a tensor's pieces, as bits (which order magnitudes, and infinities and NaNs above them).
+template <typename T> struct AbsMax {
+    uint32_t acc = 0;
+    __device__ __forceinline__ void add(const uint4& v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) acc = max(acc, w[i] & 0x7fffffffu);
+            else acc = __vmaxu2(acc, w[i] & 0x7fff7fffu);
+        }
+    }
+    __device__ __forceinline__ uint32_t bits() const { return sizeof(T) == 4 ? acc : max(acc & 0xffffu, acc >> 16); }
+};
+// Those bits as a number; not a number for infinities too.
+template <typename T>
+__device__ __forceinline__ float magnitude(uint32_t bits) {
+    float f;
+    if constexpr (sizeof(T) == 4) f = __uint_as_float(bits);
+    else f = to_f32<T>(*reinterpret_cast<const T*>(&bits));
+    return f <= 3.4028234e38f ? f : __int_as_float(0x7fc00000);
+}
 #endif
