@@ -25,18 +25,23 @@ struct RowsCfg {
     static constexpr int ROW = D * ESIZE;                    // bytes of a key
     static constexpr int CHUNKS = ROW / 16;
     static constexpr int STAGE = 2 * kKeys * ROW;            // K and V of a tile
-    static constexpr int FIT = 98304 / (kWarps * STAGE);
-    static constexpr int STAGES = FIT < 3 ? 3 : FIT > 6 ? 6 : FIT;
+    // copies on the way: a tile a warp at least while it works on another, with three blocks on an SM (one for 16-bit rows of 128)
+    static constexpr int FIT = 65536 / (kWarps * STAGE);
+    static constexpr int STAGES = FIT < 2 ? 3 : FIT > 6 ? 6 : FIT;
+    static constexpr int BLOCKS = FIT < 2 ? 1 : 3;
     static constexpr int RING = kWarps * STAGES * STAGE;
     static constexpr int MERGE = kWarps * kRowTile * D * 4;
     static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
 
-// Where 16-byte piece `c` of key `r` lies in its row: lanes that read one piece number of eight keys, or several of one, meet different banks.
+// Piece c of key r lies at piece c ^ bank_shift(r) of its row: lanes that read one piece number of eight keys, or several of one, meet
+// different banks.  (Linear over XOR in the bits of r, so that constant parts of r shift by constants.)
 template <int CHUNKS>
-__device__ __forceinline__ int swizzled(int r, int c) {
-    const int f = (((r >> 1) & 3) * 2) ^ ((r & 1) * 4);
-    return c ^ (f & (CHUNKS - 1));
+__host__ __device__ __forceinline__ constexpr int bank_shift(int r) {
+    return ((((r >> 1) & 3) * 2) ^ ((r & 1) * 4)) & (CHUNKS - 1);
+}
+__device__ __forceinline__ void cp_async_16_full(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool yes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(yes ? 16 : 0) : "memory");
@@ -107,7 +112,7 @@ struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
 // KV: type of the keys and values; BF16: type of Q and O.  part: [n_splits][B][k_h][Tq][D] sums and ml: [n_splits][B][k_h][Tq] (maximum, total),
 // where the keys are split.
 template <int KV, int D, bool BF16>
-__global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
+__global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
@@ -213,6 +218,10 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
             else return a.table[(size_t)b * a.max_pages + n / a.page];
         };
         int ahead = look_ahead(0);
+        // where this lane's first piece of a tile goes, and the distance between its pieces (32 lanes x 16 bytes: 32 / CHUNKS keys)
+        constexpr int RPI = 32 / C::CHUNKS > 0 ? 32 / C::CHUNKS : 1;
+        const int my_row = lane / C::CHUNKS, my_chunk = lane % C::CHUNKS;
+        const int my_dst = my_row * C::ROW + ((my_chunk ^ bank_shift<C::CHUNKS>(my_row)) << 4);
         auto issue = [&](int it) {
             const int tile = t0 + warp + it * kWarps;
             if (tile < t1) {
@@ -229,28 +238,42 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
                 const unsigned vis = __ballot_sync(0xffffffffu, ok);
                 if (lane == 0) meta[slot].vis = vis;
                 if (vis != 0) {
-                    if constexpr (!DENSE) {
+                    const char *kp[2], *vp[2];       // this lane's first piece among the first 16 keys, and among the others
+                    if constexpr (DENSE) {
+                        kp[0] = kbase + ((long long)(n0 + my_row) * a.ks[2] + my_chunk * 8) * 2;
+                        vp[0] = vbase + ((long long)(n0 + my_row) * a.vs[2] + my_chunk * 8) * 2;
+                    } else {
                         if ((lane & 15) == 0 && ok) {
                             const size_t ph = (size_t)ahead * a.Hk + g;
                             cp_async_4(ptx::smem_u32(&meta[slot].ks[lane >> 4]), a.k_scales + ph);
                             cp_async_4(ptx::smem_u32(&meta[slot].vs[lane >> 4]), a.v_scales + ph);
                         }
+                        const int id0 = __shfl_sync(0xffffffffu, ahead, 0), id1 = __shfl_sync(0xffffffffu, ahead, 16);
+                        const size_t o0 = (((size_t)id0 * a.Hk + g) * a.page + (n0 & (a.page - 1))) * D + lane * 16;
+                        const size_t o1 = (((size_t)id1 * a.Hk + g) * a.page + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
+                        kp[0] = kbase + o0; vp[0] = vbase + o0;
+                        kp[1] = kbase + o1; vp[1] = vbase + o1;
                     }
 #pragma unroll
                     for (int i = 0; i < C::CHUNKS; ++i) {
-                        const int p = i * 32 + lane, r = p / C::CHUNKS, c = p % C::CHUNKS;
-                        const bool yes = (vis >> r) & 1u;
-                        const uint32_t at = dst + r * C::ROW + swizzled<C::CHUNKS>(r, c) * 16;
-                        size_t ko = 0, vo = 0;
+                        const uint32_t at = dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
+                        const char *ks, *vs;
                         if constexpr (DENSE) {
-                            ko = (size_t)(n0 + r) * a.ks[2] * 2 + c * 16;
-                            vo = (size_t)(n0 + r) * a.vs[2] * 2 + c * 16;
+                            ks = kp[0] + (long long)(i * RPI) * a.ks[2] * 2;
+                            vs = vp[0] + (long long)(i * RPI) * a.vs[2] * 2;
                         } else {
-                            const int id = __shfl_sync(0xffffffffu, ahead, r);
-                            ko = vo = (((size_t)id * a.Hk + g) * a.page + (n0 + r) % a.page) * D + c * 16;
+                            const int h = C::CHUNKS == 1 ? (lane >> 4) : i >= C::CHUNKS / 2, j = C::CHUNKS == 1 ? 0 : i - h * (C::CHUNKS / 2);
+                            ks = (h ? kp[1] : kp[0]) + j * 512;
+                            vs = (h ? vp[1] : vp[0]) + j * 512;
                         }
-                        cp_async_16_or_zero(at, yes ? kbase + ko : kbase, yes);
-                        cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vbase + vo : vbase, yes);
+                        if (vis == 0xffffffffu) {
+                            cp_async_16_full(at, ks);
+                            cp_async_16_full(at + kKeys * C::ROW, vs);
+                        } else {
+                            const bool yes = (vis >> (i * RPI + my_row)) & 1u;
+                            cp_async_16_or_zero(at, yes ? ks : kbase, yes);
+                            cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vs : vbase, yes);
+                        }
                     }
                 }
                 ahead = look_ahead(it + 1);
@@ -259,6 +282,22 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
         };
 #pragma unroll
         for (int s = 0; s < C::STAGES - 1; ++s) issue(s);
+
+        // where this lane reads: K's pieces of key gq of every eight, V's pieces of keys 2 t4 and 2 t4 + 1 of every eight
+        constexpr int VB = D / 8 * C::ESIZE;                        // bytes of a key of V that a lane takes
+        constexpr int PIECE = VB < 16 ? VB : 16, PIECES = VB / PIECE, WORDS = VB < 4 ? 1 : VB / 4;
+        constexpr int KB = C::ROW / 4 < 16 ? C::ROW / 4 : 16;       // of a key of K, at a time
+        const int k_at = gq * C::ROW + ((((t4 * KB) >> 4) ^ bank_shift<C::CHUNKS>(gq)) << 4) + ((t4 * KB) & 15);
+        int v_at[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) v_at[u] = (2 * t4 + u) * C::ROW + ((((gq * VB) >> 4) ^ bank_shift<C::CHUNKS>(2 * t4 + u)) << 4) + ((gq * VB) & 15);
+        // keys below this are seen by every row of the warp
+        int all_see = min(last[0], last[1]);
+        if (!DENSE && a.causal) {
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, x));
+        }
+        float vref = 0.0f, inv_vref = 0.0f;                         // O is in units of vref (8-bit values; see below)
 
         // -------------------------------------------------------------------- tiles of 32 keys
         for (int it = 0; t0 + warp + it * kWarps < t1; ++it) {
@@ -269,64 +308,40 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
             const uint32_t kt = ring + slot * C::STAGE, vt = kt + kKeys * C::ROW;
             const unsigned vis = meta[slot].vis;
             if (vis != 0) {
+                const bool full = vis == 0xffffffffu && n0 + kKeys <= all_see;
                 // ------ scores
                 float s[4][4];
 #pragma unroll
                 for (int nt = 0; nt < 4; ++nt) {
-                    const int r = nt * 8 + gq;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) s[nt][x] = 0.0f;
-                    if constexpr (C::ROW / 4 >= 16) {
 #pragma unroll
-                        for (int c = 0; c < C::CHUNKS / 4; ++c) {
-                            uint32_t w[4];
-                            lds<16>(kt + r * C::ROW + swizzled<C::CHUNKS>(r, c * 4 + t4) * 16, w);
-                            if constexpr (DENSE) {
-                                mma16<MMA_BF16>(s[nt], qf[c * 2], w[0], w[1]);
-                                mma16<MMA_BF16>(s[nt], qf[c * 2 + 1], w[2], w[3]);
-                            } else {
+                    for (int c = 0; c < (C::CHUNKS + 3) / 4; ++c) {
+                        uint32_t w[4];
+                        lds<KB>(kt + (k_at ^ (c * 64)) + nt * 8 * C::ROW, w);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    uint32_t p01, p23;
-                                    codes_to_f16<I8>(w[x], p01, p23);
-                                    mma16<false>(s[nt], qf[c * 4 + x], p01, p23);
-                                }
-                            }
-                        }
-                    } else {
-                        constexpr int BYTES = C::ROW / 4;        // 8 or 4
-                        const int off = t4 * BYTES;
-                        uint32_t w[2];
-                        lds<BYTES>(kt + r * C::ROW + swizzled<C::CHUNKS>(r, off / 16) * 16 + off % 16, w);
-                        if constexpr (DENSE) mma16<MMA_BF16>(s[nt], qf[0], w[0], w[1]);
-                        else {
-#pragma unroll
-                            for (int x = 0; x < BYTES / 4; ++x) {
+                        for (int x = 0; x < KB / (DENSE ? 8 : 4); ++x) {
+                            if constexpr (DENSE) mma16<MMA_BF16>(s[nt], qf[c * 2 + x], w[2 * x], w[2 * x + 1]);
+                            else {
                                 uint32_t p01, p23;
                                 codes_to_f16<I8>(w[x], p01, p23);
-                                mma16<false>(s[nt], qf[x], p01, p23);
+                                mma16<false>(s[nt], qf[c * 4 + x], p01, p23);
                             }
                         }
                     }
                 }
                 // ------ softmax: element (row gq + 8 * (x >> 1), key nt * 8 + 2 t4 + (x & 1))
-                float sc[2][2];
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        if constexpr (DENSE) sc[half][u] = rscale[half];
-                        else sc[half][u] = rscale[half] * meta[slot].ks[a.page == 16 ? u : 0];
-                    }
                 float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const int n = nt * 8 + 2 * t4 + (x & 1), half = x >> 1;
-                        const bool ok = ((vis >> n) & 1u) && n0 + n < last[half];
-                        s[nt][x] = ok ? s[nt][x] * sc[half][nt >> 1] : -INFINITY;
-                        top[half] = fmaxf(top[half], s[nt][x]);
+                        s[nt][x] *= DENSE ? rscale[x >> 1] : rscale[x >> 1] * meta[slot].ks[nt >> 1];
+                        if (!full) {
+                            const int n = nt * 8 + 2 * t4 + (x & 1);
+                            if (!((vis >> n) & 1u) || n0 + n >= last[x >> 1]) s[nt][x] = -INFINITY;
+                        }
+                        top[x >> 1] = fmaxf(top[x >> 1], s[nt][x]);
                     }
                 float keep[2], ref[2];
 #pragma unroll
@@ -352,60 +367,68 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
 #pragma unroll
                         for (int x = 0; x < 4; ++x) o[j][x] *= keep[x >> 1];
                 }
-                uint32_t p[2][4], q[2][4];
+                // ------ values, 16 keys at a time: column gq * (D / 8) + j is the MMA's column gq of tile j
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
+                for (int kk = 0; kk < 2; ++kk) {
+                    if constexpr (!DENSE) {
+                        // The page's scale multiplies the weights, as a ratio to vref; where it is far from that, O changes its unit.
+                        // (A page 2^64 times smaller leaves it: its values are nothing beside what O may hold.)
+                        if (((vis >> (kk * 16)) & 0xffffu) == 0) continue;
+                        const float vs = meta[slot].vs[kk];
+                        float ratio = vs * inv_vref;
+                        if (!(fabsf(ratio) >= 0.0625f && fabsf(ratio) <= 16.0f)) {
+                            if (!(fabsf(vs) <= 3.4028234e38f)) ratio = __int_as_float(0x7fc00000);
+                            else if (fabsf(vs) >= fmaxf(1.17549435e-38f, fabsf(vref) * 5.42101086e-20f)) {
+                                const float f = vref / vs;
+#pragma unroll
+                                for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+                                    for (int x = 0; x < 4; ++x) o[j][x] *= f;
+                                vref = vs;
+                                inv_vref = 1.0f / vs;
+                                ratio = 1.0f;
+                            }
+                        }
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                float& p = s[2 * kk + y][x];
+                                // (a row that sees nothing of the page takes nothing of its scale, which may not be a number)
+                                p = full || p != 0.0f ? p * ratio : 0.0f;
+                            }
+                    }
+                    uint32_t p[4], q[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const float lo = s[2 * kk + (x >> 1)][(x & 1) * 2], hi = s[2 * kk + (x >> 1)][(x & 1) * 2 + 1];
-                        p[kk][x] = pack2<MMA_BF16>(lo, hi);
+                        p[x] = pack2<MMA_BF16>(lo, hi);
                         if constexpr (SPLIT_P) {
-                            const float2 f = unpack2<MMA_BF16>(p[kk][x]);
-                            q[kk][x] = pack2<MMA_BF16>(lo - f.x, hi - f.y);
+                            const float2 f = unpack2<MMA_BF16>(p[x]);
+                            q[x] = pack2<MMA_BF16>(lo - f.x, hi - f.y);
                         }
                     }
-                // ------ values: column gq * (D / 8) + j is the MMA's column gq of tile j
-                constexpr int VB = D / 8 * C::ESIZE;                        // bytes of a key that a lane takes
-                constexpr int PIECE = VB < 16 ? VB : 16, WORDS = VB < 4 ? 1 : VB / 4;
-                uint32_t v[2][4][WORDS];
+                    uint32_t v[4][WORDS];
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
+                    for (int x = 0; x < 4; ++x)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int r = kk * 16 + 2 * t4 + (x & 1) + (x >> 1) * 8;
+                        for (int y = 0; y < PIECES; ++y) lds<PIECE>(vt + (v_at[x & 1] ^ (y * 16)) + (kk * 16 + (x >> 1) * 8) * C::ROW, &v[x][y * 4]);
+                    if constexpr (DENSE) {
 #pragma unroll
-                        for (int y = 0; y < VB / PIECE; ++y) {
-                            const int off = gq * VB + y * PIECE;
-                            lds<PIECE>(vt + r * C::ROW + swizzled<C::CHUNKS>(r, off / 16) * 16 + off % 16, &v[kk][x][y * 4]);
-                        }
-                    }
-                if constexpr (DENSE) {
-#pragma unroll
-                    for (int j = 0; j < NTILES; ++j)
-#pragma unroll
-                        for (int kk = 0; kk < 2; ++kk) {
+                        for (int j = 0; j < NTILES; ++j) {
                             const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
-                            const uint32_t b0 = __byte_perm(v[kk][0][j / 2], v[kk][1][j / 2], sel), b1 = __byte_perm(v[kk][2][j / 2], v[kk][3][j / 2], sel);
-                            mma16<MMA_BF16>(o[j], p[kk], b0, b1);
-                            mma16<MMA_BF16>(o[j], q[kk], b0, b1);
+                            const uint32_t b0 = __byte_perm(v[0][j / 2], v[1][j / 2], sel), b1 = __byte_perm(v[2][j / 2], v[3][j / 2], sel);
+                            mma16<MMA_BF16>(o[j], p, b0, b1);
+                            mma16<MMA_BF16>(o[j], q, b0, b1);
                         }
-                } else {
-                    // a row that sees nothing of a page takes nothing of its scale either, which may not be a number
-                    float vs[2][2];
+                    } else {
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) vs[half][u] = n0 + u * 16 < last[half] && ((vis >> (u * 16)) & 0xffffu) ? meta[slot].vs[a.page == 16 ? u : 0] : 0.0f;
-#pragma unroll
-                    for (int jw = 0; jw < (NTILES + 3) / 4; ++jw) {
-                        float tmp[4][4];
-#pragma unroll
-                        for (int kk = 0; kk < 2; ++kk) {
+                        for (int jw = 0; jw < (NTILES + 3) / 4; ++jw) {
                             uint32_t b0[4], b1[4];
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
                                 uint32_t* bb = y ? b1 : b0;
-                                uint32_t w0 = v[kk][2 * y][jw], w1 = v[kk][2 * y + 1][jw];
+                                uint32_t w0 = v[2 * y][jw], w1 = v[2 * y + 1][jw];
                                 if constexpr (I8) { w0 ^= 0x80808080u; w1 ^= 0x80808080u; }
                                 const uint32_t lo = __byte_perm(w0, w1, 0x5140), hi = __byte_perm(w0, w1, 0x7362);   // (a0 b0 a1 b1), (a2 b2 a3 b3)
                                 if constexpr (I8) {
@@ -421,22 +444,21 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
                                 }
                             }
 #pragma unroll
-                            for (int jj = 0; jj < 4; ++jj) {
-                                const int j = jw * 4 + jj;
-                                if (j >= NTILES) continue;
-                                if (kk == 0 || a.page == 16) tmp[jj][0] = tmp[jj][1] = tmp[jj][2] = tmp[jj][3] = 0.0f;
-                                mma16<false>(tmp[jj], p[kk], b0[jj], b1[jj]);
-                                if constexpr (SPLIT_P) mma16<false>(tmp[jj], q[kk], b0[jj], b1[jj]);
-                                if (kk == 1 || a.page == 16) {
-#pragma unroll
-                                    for (int x = 0; x < 4; ++x) o[j][x] = fmaf(tmp[jj][x], vs[x >> 1][kk == 1 && a.page != 16 ? 0 : kk], o[j][x]);
-                                }
+                            for (int jj = 0; jj < 4 && jw * 4 + jj < NTILES; ++jj) {
+                                mma16<false>(o[jw * 4 + jj], p, b0[jj], b1[jj]);
+                                if constexpr (SPLIT_P) mma16<false>(o[jw * 4 + jj], q, b0[jj], b1[jj]);
                             }
                         }
                     }
                 }
             }
             __syncwarp();
+        }
+        if constexpr (!DENSE) {
+#pragma unroll
+            for (int j = 0; j < NTILES; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[j][x] *= vref;
         }
         ptx::cp_async_wait_all();
         // -------------------------------------------------------------------- the four warps' parts
@@ -486,14 +508,16 @@ __global__ void __launch_bounds__(kWarps * 32) kv_rows_kernel(const KvAttendArgs
     }
 }
 
-// Blocks along the keys: enough to fill the GPU twice over, each with a tile for every warp at least.
+// Blocks along the keys: as many as one wave holds, each with a tile for every warp at least.
 int rows_splits(const KvAttendArgs& a) {
+    // blocks that the GPU holds at a time (RowsCfg::BLOCKS): one wave of them
+    const long long slots = (a.format == 0 && a.d == 128 ? 1 : 3) * kSmCount;
     const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
     const long long row_tiles = ((long long)heads * a.Tq + kRowTile - 1) / kRowTile;
     const long long blocks = (long long)a.B * a.Hk * (row_tiles < 64 ? row_tiles : 64);
     const long long most = ((long long)a.Tk + kWarps * kKeys - 1) / (kWarps * kKeys);
     if (blocks == 0) return 1;
-    long long n = (2 * kSmCount + blocks - 1) / blocks;
+    long long n = slots / blocks;
     if (n > most) n = most;
     if (n > 128) n = 128;
     return n < 1 ? 1 : (int)n;

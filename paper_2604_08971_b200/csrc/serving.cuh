@@ -74,23 +74,27 @@ __device__ __forceinline__ int round_quotient_i8(float x, float s, float inv) {
     else if (e2 < -s || (e2 == -s && odd)) r -= 1.0f;
     return (int)fminf(fmaxf(r, -127.0f), 127.0f);
 }
-// Eight values over s (positive): codes as two words.  x * inv is within 127 * 2^-23 of the quotient, so that its nearest integer is the
-// quotient's unless it lies that near to a half; adding 1.5 * 2^23 rounds and leaves the integer in the low bits.
+// N values over s (positive): codes as words.  Adding 1.5 * 2^23 rounds x * inv to an integer r and leaves it in the low bits; that is one
+// off where the quotient lies next to a half (which is common: two bf16 numbers' quotient is one of few fractions).  The remainder
+// x - r s is exact, and twice it against s says so; an exact half, which has to go to the even side, is left to round_quotient_i8.
 __device__ __forceinline__ uint32_t pack_low_bytes(float a, float b, float c, float d) {
     return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 template <int N>
 __device__ __forceinline__ void codes_i8(const float (&x)[N], float s, float inv, uint32_t (&w)[N / 4]) {
     constexpr float kMagic = 12582912.0f;
-    float y[N], far = 0.0f;
+    float y[N];
+    bool half = false;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         y[i] = fmaf(x[i], inv, kMagic);
-        far = fmaxf(far, fabsf(fmaf(x[i], inv, kMagic - y[i])));
+        const float e = fmaf(kMagic - y[i], s, x[i]), d = fmaf(2.0f, fabsf(e), -s);
+        if (d > 0.0f) y[i] += copysignf(1.0f, e);
+        half = half || d == 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) w[i] = pack_low_bytes(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-    if (far > 0.4999f) {
+    if (half) {
 #pragma unroll 1
         for (int i = 0; i < N; ++i) {
             float v = x[0];
