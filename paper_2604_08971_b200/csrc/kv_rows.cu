@@ -1,20 +1,22 @@
 // Serving attention for few rows: a decoder's single tokens and short blocks, over dense 16-bit keys and values or the 8-bit cache.
 //
-// The rows of one KV group (kept heads x Tq) share its keys, so they are packed into tiles of 16 rows, and a block takes a tile and a
+// The rows of one KV group (kept heads x Tq) share its keys, so they are packed into tiles of 8 or 16 rows, and a block takes a tile and a
 // stretch of the keys.  Each of its four warps walks tiles of 32 keys by itself, with a ring of asynchronous copies of its own, a running
-// maximum and sum of its own (log2 domain), and both products on the warp MMA (16 rows x 8 keys or columns x 16): no barrier until the
-// four partial results meet.  Long axes are split over blocks; kv_combine_kernel joins the parts.
+// maximum and sum of its own (log2 domain), and both products on the warp MMA: no barrier until the four partial results meet.
+// Long axes are split over blocks; kv_combine_kernel joins the parts.
+// The keys are the MMA's 16 rows and the queries its 8 columns (S^T = K Q^T, O^T = V^T P^T): a decoder's few rows fill it, where queries as
+// rows left half of it and half of the exponentials empty (two hours of cached tokens 31 us so, with 840 instructions a tile of 4 KB).
 // What bounds it: the bytes of K and V, read once from memory.  For that the codes go through registers straight into MMA operands:
 // the order of the inner index is free as long as both operands share it, so that a lane's 16 consecutive bytes of a key are its operand
-// for K's product; and for V's, where pairs run along the keys, two keys' words are interleaved byte by byte.  8-bit codes become fp16 exactly; a page's
-// key scale multiplies the scores, its value scale the tile's product before that joins the accumulator (folded into the weights it
-// would cost fp16's range).
+// for K's product; and for V's, where pairs run along the keys, two keys' words are interleaved byte by byte.  The weights get from the
+// first product's layout to the second's by a transposition of 8 x 8 matrices among registers.  8-bit codes become fp16 exactly; a
+// page's key scale multiplies the scores, its value scale the weights.  The maximum is followed only where a score exceeds it by 2^8.
 #include "kv_attend.cuh"
 #include "ptx/sm100.cuh"
 
 namespace {
 
-constexpr int kWarps = 4, kKeys = 32, kRowTile = 16;
+constexpr int kWarps = 4, kKeys = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2, KV_I8 = 3 };
@@ -30,7 +32,7 @@ struct RowsCfg {
     static constexpr int STAGES = FIT < 2 ? 3 : FIT > 6 ? 6 : FIT;
     static constexpr int BLOCKS = FIT < 2 ? 1 : 3;
     static constexpr int RING = kWarps * STAGES * STAGE;
-    static constexpr int MERGE = kWarps * kRowTile * D * 4;
+    static constexpr int MERGE = kWarps * 16 * D * 4;
     static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
 
@@ -107,36 +109,42 @@ __device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& p01, uint32_t
     }
 }
 
+// 8 x 8 matrix of 16-bit values spread over a warp (a row's pairs over four lanes), transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
 struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
 
-// KV: type of the keys and values; BF16: type of Q and O.  part: [n_splits][B][k_h][Tq][D] sums and ml: [n_splits][B][k_h][Tq] (maximum, total),
-// where the keys are split.
-template <int KV, int D, bool BF16>
-__global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
+// KV: type of the keys and values; BF16: type of Q and O; NT: tiles of 8 rows a block takes at a time.
+// part: [n_splits][B][k_h][Tq][D] sums and ml: [n_splits][B][k_h][Tq] (maximum, total), where the keys are split.
+template <int KV, int D, bool BF16, int NT>
+__global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS)
+kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
     constexpr bool SPLIT_P = DENSE || !BF16;                 // weights as a head and a remainder
-    constexpr int KSTEPS = D / 16, NTILES = D / 8;
+    constexpr int KSTEPS = D / 16, DT = D / 16, ROWS = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ RowsMeta s_meta[kWarps][C::STAGES];
     __shared__ short s_head[kServeMaxHeads], s_pos[kServeMaxHeads];
     __shared__ int s_heads;
-    __shared__ float s_m[kWarps][kRowTile], s_l[kWarps][kRowTile];
+    __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, t4 = lane & 3;
     const int split = blockIdx.x % n_splits, bg = blockIdx.x / n_splits, b = bg / a.Hk, g = bg % a.Hk;
     grid_dependents_start_if_small();
     grid_dependency_wait();
-
-    // the kept heads of this group, in the list's order
     if (warp == 0) {
         const int n = kv_group_heads(a, b, g, g == 0 && split == 0 && blockIdx.y == 0, s_head, s_pos);
         if (lane == 0) s_heads = n;
     }
-    __syncthreads();
-    const int rows = s_heads * a.Tq;
     const int len = kv_length(a, b);
     const uint32_t mask = a.masks ? a.masks[b] : 0u;
+    __syncthreads();
+    const int rows = s_heads * a.Tq;
     const int tiles = (len + kKeys - 1) / kKeys;
     const int per_split = ((tiles + n_splits - 1) / n_splits + kWarps - 1) / kWarps * kWarps;
     const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles);
@@ -150,28 +158,109 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
         kbase = (const char*)a.K;
         vbase = (const char*)a.V;
     }
+    const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
+    const int32_t* pages = DENSE ? nullptr : a.table + (size_t)b * a.max_pages;
 
-    for (int row0 = blockIdx.y * kRowTile; row0 < rows; row0 += gridDim.y * kRowTile) {
-        // -------------------------------------------------------------------- this lane's two rows of Q as MMA operands
-        uint32_t qf[KSTEPS][4];
-        float rscale[2];
-        int last[2];                                            // keys that the row sees end here
+    for (int row0 = blockIdx.y * ROWS; row0 < rows; row0 += gridDim.y * ROWS) {
+        // -------------------------------------------------------------------- copies
+        // `ahead`: the modality id, or the page, of this lane's key of the tile that is issued next
+        auto look_ahead = [&](int tile) -> int {
+            const int n = tile * kKeys + lane;
+            if (tile >= t1 || n >= len) return -1;
+            if constexpr (DENSE) return a.ids ? a.ids[n] : 0;
+            else return pages[n >> page_shift];
+        };
+        // where this lane's first piece of a tile goes, and the distance between its pieces (32 lanes x 16 bytes: 32 / CHUNKS keys)
+        constexpr int RPI = 32 / C::CHUNKS;
+        const int my_row = lane / C::CHUNKS, my_chunk = lane % C::CHUNKS;
+        const int my_dst = my_row * C::ROW + ((my_chunk ^ bank_shift<C::CHUNKS>(my_row)) << 4);
+        int next = t0 + warp, next_slot = 0, ahead = look_ahead(next);
+        auto issue = [&]() {
+            if (next < t1) {
+                const uint32_t dst = ring + next_slot * C::STAGE;
+                RowsMeta* mt = meta + next_slot;
+                const int n0 = next * kKeys;
+                bool ok = n0 + lane < len;
+                if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
+                else {
+                    const bool good = (unsigned)ahead < (unsigned)a.n_pages;
+                    if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                    ok = ok && good;
+                }
+                const unsigned vis = __ballot_sync(0xffffffffu, ok);
+                if (lane == 0) mt->vis = vis;
+                if (vis != 0) {
+                    const char *kp[2], *vp[2];       // this lane's first piece among the first 16 keys, and among the others
+                    if constexpr (DENSE) {
+                        kp[0] = kbase + ((long long)(n0 + my_row) * a.ks[2] + my_chunk * 8) * 2;
+                        vp[0] = vbase + ((long long)(n0 + my_row) * a.vs[2] + my_chunk * 8) * 2;
+                    } else {
+                        if ((lane & 15) == 0 && ok) {
+                            const size_t ph = (size_t)ahead * a.Hk + g;
+                            cp_async_4(ptx::smem_u32(&mt->ks[lane >> 4]), a.k_scales + ph);
+                            cp_async_4(ptx::smem_u32(&mt->vs[lane >> 4]), a.v_scales + ph);
+                        }
+                        const int id0 = __shfl_sync(0xffffffffu, ahead, 0), id1 = __shfl_sync(0xffffffffu, ahead, 16);
+                        const size_t o0 = ((((size_t)id0 * a.Hk + g) << page_shift) + (n0 & (a.page - 1))) * D + lane * 16;
+                        const size_t o1 = ((((size_t)id1 * a.Hk + g) << page_shift) + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
+                        kp[0] = kbase + o0; vp[0] = vbase + o0;
+                        kp[1] = kbase + o1; vp[1] = vbase + o1;
+                    }
+                    auto piece = [&](int i, const char*& ks, const char*& vs) {
+                        if constexpr (DENSE) {
+                            ks = kp[0] + (long long)(i * RPI) * a.ks[2] * 2;
+                            vs = vp[0] + (long long)(i * RPI) * a.vs[2] * 2;
+                        } else {
+                            const int h = C::CHUNKS == 1 ? (lane >> 4) : i >= C::CHUNKS / 2, j = C::CHUNKS == 1 ? 0 : i - h * (C::CHUNKS / 2);
+                            ks = (h ? kp[1] : kp[0]) + j * 512;
+                            vs = (h ? vp[1] : vp[0]) + j * 512;
+                        }
+                        return dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
+                    };
+                    const char *ks, *vs;
+                    if (vis == 0xffffffffu) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = row0 + gq + half * 8;
+                        for (int i = 0; i < C::CHUNKS; ++i) {
+                            const uint32_t at = piece(i, ks, vs);
+                            cp_async_16_full(at, ks);
+                            cp_async_16_full(at + kKeys * C::ROW, vs);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < C::CHUNKS; ++i) {
+                            const uint32_t at = piece(i, ks, vs);
+                            const bool yes = (vis >> (i * RPI + my_row)) & 1u;
+                            cp_async_16_or_zero(at, yes ? ks : kbase, yes);
+                            cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vs : vbase, yes);
+                        }
+                    }
+                }
+                next += kWarps;
+                next_slot = next_slot + 1 == C::STAGES ? 0 : next_slot + 1;
+                ahead = look_ahead(next);
+            }
+            ptx::cp_async_commit();
+        };
+#pragma unroll
+        for (int s = 0; s < C::STAGES - 1; ++s) issue();
+
+        // -------------------------------------------------------------------- rows of Q as MMA operands: lane (gq, t4) has row gq of every eight
+        uint32_t qf[NT][KSTEPS][2];
+        float scale[NT][2];                                     // of rows 2 t4 and 2 t4 + 1, whose scores this lane will hold
+        int last[NT][2];                                        // keys that they see end here
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = row0 + nt * 8 + gq;
             const bool in = r < rows;
-            const int jj = in ? r / a.Tq : 0, i = in ? r % a.Tq : 0;
-            const char* q = (const char*)a.Q + (b * a.qs[0] + (in ? s_head[jj] : 0) * a.qs[1] + i * a.qs[2]) * 2;
-            last[half] = !DENSE && a.causal ? min(len, len - a.Tq + i + 1) : len;
-            uint32_t w[KSTEPS][2];
+            const char* q = (const char*)a.Q + (b * a.qs[0] + (in ? s_head[r / a.Tq] : 0) * a.qs[1] + (in ? r % a.Tq : 0) * a.qs[2]) * 2;
             // elements of a chunk that one lane has: 16 bytes of a key, or a quarter of a shorter one
             constexpr int E = (C::ROW / 4 < 16 ? C::ROW / 4 : 16) / C::ESIZE;
 #pragma unroll
             for (int s = 0; s < KSTEPS; ++s) {
                 const int e = (s / (E / 4)) * 4 * E + t4 * E + (s % (E / 4)) * 4;
                 const uint2 x = in ? *reinterpret_cast<const uint2*>(q + e * 2) : make_uint2(0, 0);
-                w[s][0] = x.x;
-                w[s][1] = x.y;
+                qf[nt][s][0] = x.x;
+                qf[nt][s][1] = x.y;
             }
             float rs = rsqrtf((float)D) * kLog2e;
             if constexpr (!DENSE && BF16) {
@@ -181,7 +270,7 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
                 for (int s = 0; s < KSTEPS; ++s)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float2 f = unpack2<true>(w[s][x]);
+                        const float2 f = unpack2<true>(qf[nt][s][x]);
                         top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
                     }
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -194,95 +283,27 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
                 for (int s = 0; s < KSTEPS; ++s)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float2 f = unpack2<true>(w[s][x]);
-                        w[s][x] = pack2<false>(f.x * down, f.y * down);
+                        const float2 f = unpack2<true>(qf[nt][s][x]);
+                        qf[nt][s][x] = pack2<false>(f.x * down, f.y * down);
                     }
             }
-            rscale[half] = rs;
 #pragma unroll
-            for (int s = 0; s < KSTEPS; ++s) { qf[s][half] = w[s][0]; qf[s][2 + half] = w[s][1]; }
+            for (int x = 0; x < 2; ++x) {
+                scale[nt][x] = __shfl_sync(0xffffffffu, rs, (2 * t4 + x) * 4);
+                const int i = (row0 + nt * 8 + 2 * t4 + x) % a.Tq;
+                last[nt][x] = !DENSE && a.causal ? min(len, len - a.Tq + i + 1) : len;
+            }
         }
-        float o[NTILES][4];
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        float o[DT][NT][4], m[NT][2], l[NT][2];
 #pragma unroll
-        for (int j = 0; j < NTILES; ++j)
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[j][x] = 0.0f;
-
-        // -------------------------------------------------------------------- copies
-        // `ahead`: the modality id, or the page, of this lane's key of the tile that is issued next
-        auto look_ahead = [&](int it) -> int {
-            const int n = (t0 + warp + it * kWarps) * kKeys + lane;
-            if (t0 + warp + it * kWarps >= t1 || n >= len) return -1;
-            if constexpr (DENSE) return a.ids ? a.ids[n] : 0;
-            else return a.table[(size_t)b * a.max_pages + n / a.page];
-        };
-        int ahead = look_ahead(0);
-        // where this lane's first piece of a tile goes, and the distance between its pieces (32 lanes x 16 bytes: 32 / CHUNKS keys)
-        constexpr int RPI = 32 / C::CHUNKS > 0 ? 32 / C::CHUNKS : 1;
-        const int my_row = lane / C::CHUNKS, my_chunk = lane % C::CHUNKS;
-        const int my_dst = my_row * C::ROW + ((my_chunk ^ bank_shift<C::CHUNKS>(my_row)) << 4);
-        auto issue = [&](int it) {
-            const int tile = t0 + warp + it * kWarps;
-            if (tile < t1) {
-                const int slot = it % C::STAGES;
-                const uint32_t dst = ring + slot * C::STAGE;
-                const int n0 = tile * kKeys;
-                bool ok = n0 + lane < len;
-                if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
-                else {
-                    const bool good = ahead >= 0 && ahead < a.n_pages;
-                    if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
-                    ok = ok && good;
-                }
-                const unsigned vis = __ballot_sync(0xffffffffu, ok);
-                if (lane == 0) meta[slot].vis = vis;
-                if (vis != 0) {
-                    const char *kp[2], *vp[2];       // this lane's first piece among the first 16 keys, and among the others
-                    if constexpr (DENSE) {
-                        kp[0] = kbase + ((long long)(n0 + my_row) * a.ks[2] + my_chunk * 8) * 2;
-                        vp[0] = vbase + ((long long)(n0 + my_row) * a.vs[2] + my_chunk * 8) * 2;
-                    } else {
-                        if ((lane & 15) == 0 && ok) {
-                            const size_t ph = (size_t)ahead * a.Hk + g;
-                            cp_async_4(ptx::smem_u32(&meta[slot].ks[lane >> 4]), a.k_scales + ph);
-                            cp_async_4(ptx::smem_u32(&meta[slot].vs[lane >> 4]), a.v_scales + ph);
-                        }
-                        const int id0 = __shfl_sync(0xffffffffu, ahead, 0), id1 = __shfl_sync(0xffffffffu, ahead, 16);
-                        const size_t o0 = (((size_t)id0 * a.Hk + g) * a.page + (n0 & (a.page - 1))) * D + lane * 16;
-                        const size_t o1 = (((size_t)id1 * a.Hk + g) * a.page + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
-                        kp[0] = kbase + o0; vp[0] = vbase + o0;
-                        kp[1] = kbase + o1; vp[1] = vbase + o1;
-                    }
+            for (int j = 0; j < DT; ++j)
 #pragma unroll
-                    for (int i = 0; i < C::CHUNKS; ++i) {
-                        const uint32_t at = dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
-                        const char *ks, *vs;
-                        if constexpr (DENSE) {
-                            ks = kp[0] + (long long)(i * RPI) * a.ks[2] * 2;
-                            vs = vp[0] + (long long)(i * RPI) * a.vs[2] * 2;
-                        } else {
-                            const int h = C::CHUNKS == 1 ? (lane >> 4) : i >= C::CHUNKS / 2, j = C::CHUNKS == 1 ? 0 : i - h * (C::CHUNKS / 2);
-                            ks = (h ? kp[1] : kp[0]) + j * 512;
-                            vs = (h ? vp[1] : vp[0]) + j * 512;
-                        }
-                        if (vis == 0xffffffffu) {
-                            cp_async_16_full(at, ks);
-                            cp_async_16_full(at + kKeys * C::ROW, vs);
-                        } else {
-                            const bool yes = (vis >> (i * RPI + my_row)) & 1u;
-                            cp_async_16_or_zero(at, yes ? ks : kbase, yes);
-                            cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vs : vbase, yes);
-                        }
-                    }
-                }
-                ahead = look_ahead(it + 1);
-            }
-            ptx::cp_async_commit();
-        };
-#pragma unroll
-        for (int s = 0; s < C::STAGES - 1; ++s) issue(s);
-
+                for (int x = 0; x < 4; ++x) o[j][nt][x] = 0.0f;
+        }
         // where this lane reads: K's pieces of key gq of every eight, V's pieces of keys 2 t4 and 2 t4 + 1 of every eight
         constexpr int VB = D / 8 * C::ESIZE;                        // bytes of a key of V that a lane takes
         constexpr int PIECE = VB < 16 ? VB : 16, PIECES = VB / PIECE, WORDS = VB < 4 ? 1 : VB / 4;
@@ -292,82 +313,115 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
 #pragma unroll
         for (int u = 0; u < 2; ++u) v_at[u] = (2 * t4 + u) * C::ROW + ((((gq * VB) >> 4) ^ bank_shift<C::CHUNKS>(2 * t4 + u)) << 4) + ((gq * VB) & 15);
         // keys below this are seen by every row of the warp
-        int all_see = min(last[0], last[1]);
+        int all_see = len;
         if (!DENSE && a.causal) {
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) all_see = min(all_see, __shfl_xor_sync(0xffffffffu, all_see, x));
+            for (int nt = 0; nt < NT; ++nt) all_see = min(all_see, min(last[nt][0], last[nt][1]));
+            all_see = __reduce_min_sync(0xffffffffu, all_see);
         }
         float vref = 0.0f, inv_vref = 0.0f;                         // O is in units of vref (8-bit values; see below)
 
         // -------------------------------------------------------------------- tiles of 32 keys
-        for (int it = 0; t0 + warp + it * kWarps < t1; ++it) {
-            issue(it + C::STAGES - 1);
+        int slot = 0;
+        for (int tile = t0 + warp; tile < t1; tile += kWarps) {
+            issue();
             ptx::cp_async_wait_group<C::STAGES - 1>();
             __syncwarp();
-            const int slot = it % C::STAGES, n0 = (t0 + warp + it * kWarps) * kKeys;
+            const int n0 = tile * kKeys;
             const uint32_t kt = ring + slot * C::STAGE, vt = kt + kKeys * C::ROW;
             const unsigned vis = meta[slot].vis;
             if (vis != 0) {
                 const bool full = vis == 0xffffffffu && n0 + kKeys <= all_see;
-                // ------ scores
-                float s[4][4];
+                // ------ scores: element (key mt * 16 + gq + 8 * (x >> 1), row nt * 8 + 2 t4 + (x & 1))
+                float s[2][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt) {
+                for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) s[nt][x] = 0.0f;
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) s[mt][nt][x] = 0.0f;
 #pragma unroll
                     for (int c = 0; c < (C::CHUNKS + 3) / 4; ++c) {
-                        uint32_t w[4];
-                        lds<KB>(kt + (k_at ^ (c * 64)) + nt * 8 * C::ROW, w);
+                        uint32_t w0[4], w1[4];                      // keys gq and gq + 8
+                        lds<KB>(kt + (k_at ^ (c * 64)) + mt * 16 * C::ROW, w0);
+                        lds<KB>(kt + (k_at ^ (c * 64)) + (mt * 16 + 8) * C::ROW, w1);
 #pragma unroll
                         for (int x = 0; x < KB / (DENSE ? 8 : 4); ++x) {
-                            if constexpr (DENSE) mma16<MMA_BF16>(s[nt], qf[c * 2 + x], w[2 * x], w[2 * x + 1]);
+                            uint32_t f[4];
+                            if constexpr (DENSE) { f[0] = w0[2 * x]; f[1] = w1[2 * x]; f[2] = w0[2 * x + 1]; f[3] = w1[2 * x + 1]; }
                             else {
-                                uint32_t p01, p23;
-                                codes_to_f16<I8>(w[x], p01, p23);
-                                mma16<false>(s[nt], qf[c * 4 + x], p01, p23);
+                                codes_to_f16<I8>(w0[x], f[0], f[2]);
+                                codes_to_f16<I8>(w1[x], f[1], f[3]);
                             }
+                            constexpr int PER = KB / (DENSE ? 8 : 4);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16<MMA_BF16>(s[mt][nt], f, qf[nt][c * PER + x][0], qf[nt][c * PER + x][1]);
                         }
                     }
                 }
-                // ------ softmax: element (row gq + 8 * (x >> 1), key nt * 8 + 2 t4 + (x & 1))
-                float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
+                for (int mt = 0; mt < 2; ++mt) {
+                    const float ks = DENSE ? 1.0f : meta[slot].ks[mt];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        s[nt][x] *= DENSE ? rscale[x >> 1] : rscale[x >> 1] * meta[slot].ks[nt >> 1];
-                        if (!full) {
-                            const int n = nt * 8 + 2 * t4 + (x & 1);
-                            if (!((vis >> n) & 1u) || n0 + n >= last[x >> 1]) s[nt][x] = -INFINITY;
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float c0 = scale[nt][0] * ks, c1 = scale[nt][1] * ks;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) s[mt][nt][x] *= x & 1 ? c1 : c0;
+                    }
+                }
+                if (!full) {
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int n = mt * 16 + gq + (x >> 1) * 8;
+                            const bool here = (vis >> n) & 1u;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+                                if (!here || n0 + n >= last[nt][x & 1]) s[mt][nt][x] = -INFINITY;
                         }
-                        top[x >> 1] = fmaxf(top[x >> 1], s[nt][x]);
-                    }
-                float keep[2], ref[2];
+                }
+                // ------ softmax
+                bool over = false;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
-                    top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
-                    const float now = fmaxf(m[half], top[half]);
-                    ref[half] = now == -INFINITY ? 0.0f : now;
-                    keep[half] = exp2_fast(m[half] - ref[half]);
-                    m[half] = now;
-                    l[half] *= keep[half];
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float top = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
+                        over = over || top - m[nt][x] > 8.0f;
+                    }
+                if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float keep[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            float top = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
+#pragma unroll
+                            for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+                            top = fmaxf(top, m[nt][x]);
+                            keep[x] = top == m[nt][x] ? 1.0f : exp2_fast(m[nt][x] - top);
+                            m[nt][x] = top;
+                            l[nt][x] *= keep[x];
+                        }
+#pragma unroll
+                        for (int j = 0; j < DT; ++j)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) o[j][nt][x] *= keep[x & 1];
+                    }
                 }
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float ref[2] = {m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m[nt][1] == -INFINITY ? 0.0f : m[nt][1]};
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        s[nt][x] = exp2_fast(s[nt][x] - ref[x >> 1]);
-                        l[x >> 1] += s[nt][x];
-                    }
-                if (__any_sync(0xffffffffu, keep[0] != 1.0f || keep[1] != 1.0f)) {
+                    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int j = 0; j < NTILES; ++j)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) o[j][x] *= keep[x >> 1];
+                        for (int x = 0; x < 4; ++x) {
+                            s[mt][nt][x] = exp2_fast(s[mt][nt][x] - ref[x & 1]);
+                            l[nt][x & 1] += s[mt][nt][x];
+                        }
                 }
-                // ------ values, 16 keys at a time: column gq * (D / 8) + j is the MMA's column gq of tile j
+                // ------ values, 16 keys at a time: column gq * (D / 8) + 2 j is row gq of the MMA's tile j, the next column its row gq + 8
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
                     if constexpr (!DENSE) {
@@ -381,105 +435,111 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
                             else if (fabsf(vs) >= fmaxf(1.17549435e-38f, fabsf(vref) * 5.42101086e-20f)) {
                                 const float f = vref / vs;
 #pragma unroll
-                                for (int j = 0; j < NTILES; ++j)
+                                for (int j = 0; j < DT; ++j)
 #pragma unroll
-                                    for (int x = 0; x < 4; ++x) o[j][x] *= f;
+                                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                        for (int x = 0; x < 4; ++x) o[j][nt][x] *= f;
                                 vref = vs;
                                 inv_vref = 1.0f / vs;
                                 ratio = 1.0f;
                             }
                         }
+                        if (full) {
 #pragma unroll
-                        for (int y = 0; y < 2; ++y)
+                            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                float& p = s[2 * kk + y][x];
-                                // (a row that sees nothing of the page takes nothing of its scale, which may not be a number)
-                                p = full || p != 0.0f ? p * ratio : 0.0f;
-                            }
-                    }
-                    uint32_t p[4], q[4];
+                                for (int x = 0; x < 4; ++x) s[kk][nt][x] *= ratio;
+                        } else {
+                            // (a row that sees nothing of the page takes nothing of its scale, which may not be a number)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const float lo = s[2 * kk + (x >> 1)][(x & 1) * 2], hi = s[2 * kk + (x >> 1)][(x & 1) * 2 + 1];
-                        p[x] = pack2<MMA_BF16>(lo, hi);
-                        if constexpr (SPLIT_P) {
-                            const float2 f = unpack2<MMA_BF16>(p[x]);
-                            q[x] = pack2<MMA_BF16>(lo - f.x, hi - f.y);
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) s[kk][nt][x] = s[kk][nt][x] != 0.0f ? s[kk][nt][x] * ratio : 0.0f;
                         }
                     }
+                    uint32_t p[NT][2], q[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float x0 = s[kk][nt][2 * y], x1 = s[kk][nt][2 * y + 1];
+                            const uint32_t w = pack2<MMA_BF16>(x0, x1);
+                            p[nt][y] = transposed(w);
+                            if constexpr (SPLIT_P) {
+                                const float2 f = unpack2<MMA_BF16>(w);
+                                q[nt][y] = transposed(pack2<MMA_BF16>(x0 - f.x, x1 - f.y));
+                            }
+                        }
                     uint32_t v[4][WORDS];
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
 #pragma unroll
                         for (int y = 0; y < PIECES; ++y) lds<PIECE>(vt + (v_at[x & 1] ^ (y * 16)) + (kk * 16 + (x >> 1) * 8) * C::ROW, &v[x][y * 4]);
+                    auto product = [&](int j, const uint32_t (&f)[4]) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma16<MMA_BF16>(o[j][nt], f, p[nt][0], p[nt][1]);
+                            if constexpr (SPLIT_P) mma16<MMA_BF16>(o[j][nt], f, q[nt][0], q[nt][1]);
+                        }
+                    };
                     if constexpr (DENSE) {
 #pragma unroll
-                        for (int j = 0; j < NTILES; ++j) {
-                            const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
-                            const uint32_t b0 = __byte_perm(v[0][j / 2], v[1][j / 2], sel), b1 = __byte_perm(v[2][j / 2], v[3][j / 2], sel);
-                            mma16<MMA_BF16>(o[j], p, b0, b1);
-                            mma16<MMA_BF16>(o[j], q, b0, b1);
+                        for (int j = 0; j < DT; ++j) {
+                            const uint32_t f[4] = {__byte_perm(v[0][j], v[1][j], 0x5410), __byte_perm(v[0][j], v[1][j], 0x7632), __byte_perm(v[2][j], v[3][j], 0x5410),
+                                                   __byte_perm(v[2][j], v[3][j], 0x7632)};
+                            product(j, f);
                         }
                     } else {
 #pragma unroll
-                        for (int jw = 0; jw < (NTILES + 3) / 4; ++jw) {
-                            uint32_t b0[4], b1[4];
+                        for (int jw = 0; jw < WORDS; ++jw) {
+                            uint32_t f[2][4];
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
-                                uint32_t* bb = y ? b1 : b0;
                                 uint32_t w0 = v[2 * y][jw], w1 = v[2 * y + 1][jw];
                                 if constexpr (I8) { w0 ^= 0x80808080u; w1 ^= 0x80808080u; }
                                 const uint32_t lo = __byte_perm(w0, w1, 0x5140), hi = __byte_perm(w0, w1, 0x7362);   // (a0 b0 a1 b1), (a2 b2 a3 b3)
                                 if constexpr (I8) {
-                                    bb[0] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4140));
-                                    bb[1] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4342));
-                                    bb[2] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4140));
-                                    bb[3] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4342));
+                                    f[0][2 * y] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4140));
+                                    f[0][2 * y + 1] = biased_to_f16x2(__byte_perm(lo, 0x64646464u, 0x4342));
+                                    f[1][2 * y] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4140));
+                                    f[1][2 * y + 1] = biased_to_f16x2(__byte_perm(hi, 0x64646464u, 0x4342));
                                 } else {
-                                    bb[0] = e4m3x2_to_f16x2(lo);
-                                    bb[1] = e4m3x2_hi_to_f16x2(lo);
-                                    bb[2] = e4m3x2_to_f16x2(hi);
-                                    bb[3] = e4m3x2_hi_to_f16x2(hi);
+                                    f[0][2 * y] = e4m3x2_to_f16x2(lo);
+                                    f[0][2 * y + 1] = e4m3x2_hi_to_f16x2(lo);
+                                    f[1][2 * y] = e4m3x2_to_f16x2(hi);
+                                    f[1][2 * y + 1] = e4m3x2_hi_to_f16x2(hi);
                                 }
                             }
-#pragma unroll
-                            for (int jj = 0; jj < 4 && jw * 4 + jj < NTILES; ++jj) {
-                                mma16<false>(o[jw * 4 + jj], p, b0[jj], b1[jj]);
-                                if constexpr (SPLIT_P) mma16<false>(o[jw * 4 + jj], q, b0[jj], b1[jj]);
-                            }
+                            product(jw * 2, f[0]);
+                            if (jw * 2 + 1 < DT) product(jw * 2 + 1, f[1]);
                         }
                     }
                 }
             }
+            slot = slot + 1 == C::STAGES ? 0 : slot + 1;
             __syncwarp();
-        }
-        if constexpr (!DENSE) {
-#pragma unroll
-            for (int j = 0; j < NTILES; ++j)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[j][x] *= vref;
         }
         ptx::cp_async_wait_all();
         // -------------------------------------------------------------------- the four warps' parts
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
-            l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
-        }
         __syncthreads();                       // every ring has been read
         float* so = reinterpret_cast<float*>(smem);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = gq + half * 8;
-            if (t4 == 0) { s_m[warp][r] = m[half]; s_l[warp][r] = l[half]; }
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < NTILES; ++j)
+            for (int x = 0; x < 2; ++x) {
+                const int r = nt * 8 + 2 * t4 + x;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) so[(warp * kRowTile + r) * D + (2 * t4 + x) * (D / 8) + j] = o[j][half * 2 + x];
-        }
+                for (int y = 4; y < 32; y <<= 1) l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], y);
+                if (gq == 0) { s_m[warp][r] = m[nt][x]; s_l[warp][r] = l[nt][x]; }
+#pragma unroll
+                for (int j = 0; j < DT; ++j) {
+                    const float f = DENSE ? 1.0f : vref;
+                    *reinterpret_cast<float2*>(so + (warp * ROWS + r) * D + gq * (D / 8) + 2 * j) = make_float2(o[j][nt][x] * f, o[j][nt][x + 2] * f);
+                }
+            }
         __syncthreads();
-        for (int e = threadIdx.x; e < kRowTile * D / 2; e += kWarps * 32) {
+        for (int e = threadIdx.x; e < ROWS * D / 2; e += kWarps * 32) {
             const int r = e / (D / 2), c = e % (D / 2) * 2, row = row0 + r;
             if (row >= rows) break;
             float top = -INFINITY;
@@ -490,9 +550,10 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = exp2_fast(s_m[w][r] - ref);
+                const float2 v = *reinterpret_cast<const float2*>(so + (w * ROWS + r) * D + c);
                 sum += s_l[w][r] * f;
-                x += so[(w * kRowTile + r) * D + c] * f;
-                y += so[(w * kRowTile + r) * D + c + 1] * f;
+                x += v.x * f;
+                y += v.y * f;
             }
             const size_t out = ((size_t)b * a.k_h + s_pos[row / a.Tq]) * a.Tq + row % a.Tq;
             if (n_splits == 1) {
@@ -508,13 +569,21 @@ __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS) kv_rows_k
     }
 }
 
+// Tiles of rows: 8 where a group has no more, else 16.
+int rows_tile(const KvAttendArgs& a) {
+    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
+    return (long long)heads * a.Tq <= 8 ? 8 : 16;
+}
+long long rows_tiles(const KvAttendArgs& a) {
+    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h, tile = rows_tile(a);
+    const long long n = ((long long)heads * a.Tq + tile - 1) / tile;
+    return n < 64 ? n : 64;
+}
 // Blocks along the keys: as many as one wave holds, each with a tile for every warp at least.
 int rows_splits(const KvAttendArgs& a) {
-    // blocks that the GPU holds at a time (RowsCfg::BLOCKS): one wave of them
+    // blocks that the GPU holds at a time (RowsCfg::BLOCKS)
     const long long slots = (a.format == 0 && a.d == 128 ? 1 : 3) * kSmCount;
-    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
-    const long long row_tiles = ((long long)heads * a.Tq + kRowTile - 1) / kRowTile;
-    const long long blocks = (long long)a.B * a.Hk * (row_tiles < 64 ? row_tiles : 64);
+    const long long blocks = (long long)a.B * a.Hk * rows_tiles(a);
     const long long most = ((long long)a.Tk + kWarps * kKeys - 1) / (kWarps * kKeys);
     if (blocks == 0) return 1;
     long long n = slots / blocks;
@@ -523,11 +592,9 @@ int rows_splits(const KvAttendArgs& a) {
     return n < 1 ? 1 : (int)n;
 }
 
-template <int KV, int D, bool BF16>
+template <int KV, int D, bool BF16, int NT>
 int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     using C = RowsCfg<KV, D>;
-    const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
-    const long long row_tiles = ((long long)heads * a.Tq + kRowTile - 1) / kRowTile;
     const int n_splits = rows_splits(a);
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     float* part = nullptr;
@@ -537,27 +604,28 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
         ml = ws.take<float2>(n_splits * rows);
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
-    auto k = kv_rows_kernel<KV, D, BF16>;
+    auto k = kv_rows_kernel<KV, D, BF16, NT>;
     static std::atomic<unsigned long long> allowed{0};
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
-        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)(row_tiles < 64 ? row_tiles : 64)), dim3(kWarps * 32), C::SMEM, st, a,
-                                       part, ml, n_splits));
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)rows_tiles(a)), dim3(kWarps * 32), C::SMEM, st, a, part, ml, n_splits));
     }
-    if (n_splits > 1) {
-        return launch_kv_combine(ctx, a, part, ml, n_splits, st);
-    }
-    return SENTRY_OK;
+    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
+}
+
+template <int KV, int D, bool BF16>
+int launch_nt(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    return rows_tile(a) == 8 ? launch_rows<KV, D, BF16, 1>(ctx, a, ws, st) : launch_rows<KV, D, BF16, 2>(ctx, a, ws, st);
 }
 
 template <int KV, bool BF16>
 int launch_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     switch (a.d) {
-        case 16: return launch_rows<KV, 16, BF16>(ctx, a, ws, st);
-        case 32: return launch_rows<KV, 32, BF16>(ctx, a, ws, st);
-        case 64: return launch_rows<KV, 64, BF16>(ctx, a, ws, st);
-        default: return launch_rows<KV, 128, BF16>(ctx, a, ws, st);
+        case 16: return launch_nt<KV, 16, BF16>(ctx, a, ws, st);
+        case 32: return launch_nt<KV, 32, BF16>(ctx, a, ws, st);
+        case 64: return launch_nt<KV, 64, BF16>(ctx, a, ws, st);
+        default: return launch_nt<KV, 128, BF16>(ctx, a, ws, st);
     }
 }
 
