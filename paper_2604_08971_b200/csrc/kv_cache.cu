@@ -84,32 +84,31 @@ __global__ void __launch_bounds__(kAppThreads, 2) cache_append_kernel(const Appe
     const int start = max(at * page, len);                 // position of its first new token
     int total = most;                                      // present tokens of the sample
     if (a.ids != nullptr) {
+        // a warp counts a stretch of the tokens, then notes those of its own that this page takes
         const uint32_t mask = a.masks[b];
-        const int per = (most + kAppThreads - 1) / kAppThreads;
-        const int t0 = min((int)threadIdx.x * per, most), t1 = min(t0 + per, most);
+        const int per = ((most + kAppThreads - 1) / kAppThreads) * 32;
+        const int w0 = min(warp * per, most), w1 = min(w0 + per, most);
+        auto here = [&](int t) {
+            const int m = t < w1 ? a.ids[t] : -1;
+            return __ballot_sync(0xffffffffu, (unsigned)m < 32u && ((mask >> (m & 31)) & 1u));
+        };
         int mine = 0;
-        for (int t = t0; t < t1; ++t) {
-            const int m = a.ids[t];
-            mine += m >= 0 && m < 32 && ((mask >> m) & 1u);
-        }
-        int incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (lane == 31) s_count[warp] = incl;
+#pragma unroll 4
+        for (int t = w0; t < w1; t += 32) mine += __popc(here(t + lane));
+        if (lane == 0) s_count[warp] = mine;
         __syncthreads();
-        int before = incl - mine;
+        int r = 0;
         total = 0;
-        for (int w = 0; w < kAppThreads / 32; ++w) { if (w < warp) before += s_count[w]; total += s_count[w]; }
+#pragma unroll
+        for (int w = 0; w < kAppThreads / 32; ++w) { if (w < warp) r += s_count[w]; total += s_count[w]; }
         const int r0 = start - len;
-        for (int t = t0, r = before; t < t1 && r < r0 + page; ++t) {
-            const int m = a.ids[t];
-            if (!(m >= 0 && m < 32 && ((mask >> m) & 1u))) continue;
-            if (r >= r0) s_token[r - r0] = t;
-            ++r;
-        }
+        if (r < r0 + page && r + mine > r0)
+            for (int t = w0; t < w1 && r < r0 + page; t += 32) {
+                const unsigned bits = here(t + lane);
+                const int at_rank = r + __popc(bits & ((1u << lane) - 1u)) - r0;
+                if (((bits >> lane) & 1u) && at_rank >= 0 && at_rank < page) s_token[at_rank] = t + lane;
+                r += __popc(bits);
+            }
     }
     const int room = sane ? cap - len : 0, put = min(total, room);
     if (pb == 0 && threadIdx.x == 0) {
@@ -145,7 +144,7 @@ __global__ void __launch_bounds__(kAppThreads, 2) cache_append_kernel(const Appe
         for (int p = kHold * 32 + lane; p < pieces; p += 32) top.add(piece(p));
         const float most = magnitude<T>(__reduce_max_sync(0xffffffffu, top.bits()));
         const float now = isnan(most) || isnan(old) ? nan_f32() : fmaxf(page_scale<I8>(most), old);
-        const float inv = now > 0.0f ? __fdiv_rn(1.0f, now) : 0.0f;
+        const float inv = !(now > 0.0f) ? 0.0f : I8 && now != old ? reciprocal_i8(now, most) : __fdiv_rn(1.0f, now);
         // older codes of the page under its new scale
         if (slot0 > 0 && !(now == old))
             for (int i = lane; i < slot0 * d; i += 32) codes[i] = again<I8>(codes[i], old, now);

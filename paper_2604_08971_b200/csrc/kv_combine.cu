@@ -3,34 +3,36 @@
 
 namespace {
 
+constexpr int kMaxParts = 512;     // of a row: at most the blocks of a wave
+
 // A block per row: its warps take every fourth part, with the loads of several on the way, and meet in shared memory.  (A warp per row, part
 // after part: 37 us for 16 rows of 128 parts.)
 template <bool BF16>
-__global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int n_splits) {
-    __shared__ float s_weight[128], s_acc[4][128];
+__global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, const int2* __restrict__ plan,
+                                                         int n_splits) {
+    __shared__ float s_weight[kMaxParts], s_acc[4][128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const size_t rows = (size_t)a.B * a.k_h * a.Tq, row = blockIdx.x;
+    const size_t row = blockIdx.x, each = (size_t)a.k_h * a.Tq;      // rows of a sample
     grid_dependency_wait();
-    const int j = (int)(row / a.Tq % a.k_h), b = (int)(row / a.Tq / a.k_h);
-    if (kv_head(a, b, j) < 0) return;         // (its zero rows are written)
-    // every warp by itself: the maximum, the total, and the weights of all parts (128 at most)
-    float2 x[4];
+    const int b = (int)(row / each);
+    const size_t in = row - (size_t)b * each;
+    const int2 mine = plan != nullptr ? plan[b] : make_int2(b * n_splits, n_splits);
+    const int n = min(mine.y, kMaxParts);
+    if (plan != nullptr && n == 1) return;              // (written where it was computed)
+    if (kv_head(a, b, (int)(in / a.Tq)) < 0) return;    // (its zero rows are written)
+    // every warp by itself: the maximum, the total, and the weights of all parts
+    const float2* x0 = ml + (size_t)mine.x * each + in;
     float top = -INFINITY, total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int s = i * 32 + lane;
-        x[i] = s < n_splits ? ml[s * rows + row] : make_float2(-INFINITY, 0.0f);
-        top = fmaxf(top, x[i].x);
-    }
+    for (int s = lane; s < n; s += 32) top = fmaxf(top, x0[s * each].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float f = exp2_fast(x[i].x - ref);
-        total += x[i].y * f;
-        // (a part that saw nothing was not written)
-        if (warp == 0 && i * 32 + lane < n_splits) s_weight[i * 32 + lane] = x[i].x == -INFINITY && x[i].y == 0.0f ? -1.0f : f;
+    for (int s = lane; s < n; s += 32) {
+        const float2 x = x0[s * each];
+        const float f = exp2_fast(x.x - ref);
+        total += x.y * f;
+        // (a part that saw nothing may not have been written)
+        if (warp == 0) s_weight[s] = x.x == -INFINITY && x.y == 0.0f ? -1.0f : f;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
@@ -39,10 +41,10 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, c
     const int lanes = a.d / 4, sub = lane / lanes, subs = 32 / lanes, c = lane % lanes;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-    for (int s = warp * subs + sub; s < n_splits; s += 4 * subs) {
+    for (int s = warp * subs + sub; s < n; s += 4 * subs) {
         const float f = s_weight[s];
         if (f < 0.0f) continue;
-        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + row) * a.d + c * 4);
+        const float4 v = *reinterpret_cast<const float4*>(part + ((mine.x + s) * each + in) * a.d + c * 4);
         acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
     }
     for (int o = lanes; o < 32; o <<= 1) {
@@ -62,10 +64,10 @@ __global__ void __launch_bounds__(128) kv_combine_kernel(const KvAttendArgs a, c
 
 }  // namespace
 
-int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, int n_splits, cudaStream_t st) {
+int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, const int2* plan, int n_splits, cudaStream_t st) {
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     LaunchScope ls(ctx, KS_KV_COMBINE, st);
     auto k = a.dtype == SENTRY_BF16 ? kv_combine_kernel<true> : kv_combine_kernel<false>;
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)rows), dim3(128), 0, st, a, part, ml, n_splits));
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)rows), dim3(128), 0, st, a, part, ml, plan, n_splits));
     return SENTRY_OK;
 }

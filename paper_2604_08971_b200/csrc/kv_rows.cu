@@ -118,11 +118,48 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 
 struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
 
+// Which stretch of which sample's keys a block takes.  The samples' lengths differ and only the device knows them, so that every block works
+// out the same shares: stretches of `chunk` tiles, as many blocks to a sample as it has of them (one at least), so that all fit one wave.
+struct RowsShare { int b, split, n, first; };   // first: number of the sample's first part among all samples' parts
+__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room, int& chunk) {
+    const int lane = threadIdx.x & 31;
+    auto tiles_of = [&](int b) { return b < a.B ? (kv_length(a, b) + kKeys - 1) / kKeys : 0; };
+    int sum = 0;
+#pragma unroll 4
+    for (int b0 = 0; b0 < a.B; b0 += 32) sum += tiles_of(b0 + lane);
+    const long long total = (long long)__reduce_add_sync(0xffffffffu, sum >> 8) * 256 + __reduce_add_sync(0xffffffffu, sum & 255);
+    chunk = (int)((total + room - 1) / room);
+    chunk = max((chunk + kWarps - 1) / kWarps * kWarps, kWarps);
+    RowsShare r = {-1, 0, 0, 0};
+    int base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        const int b = b0 + lane, n = b < a.B ? max(1, (tiles_of(b) + chunk - 1) / chunk) : 0;
+        int incl = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, unit >= base + incl - n && unit < base + incl);
+        if (hit) {
+            const int who = __ffs(hit) - 1;
+            r.b = b0 + who;
+            r.first = base + __shfl_sync(0xffffffffu, incl - n, who);
+            r.n = __shfl_sync(0xffffffffu, n, who);
+            r.split = unit - r.first;
+            break;
+        }
+        base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return r;
+}
+
 // KV: type of the keys and values; BF16: type of Q and O; NT: tiles of 8 rows a block takes at a time.
-// part: [n_splits][B][k_h][Tq][D] sums and ml: [n_splits][B][k_h][Tq] (maximum, total), where the keys are split.
+// room: 0: a block per group and row tile takes all of its keys.  Otherwise the keys are shared out (rows_share), part: [parts][k_h][Tq][D] sums,
+// ml: [parts][k_h][Tq] (maximum, total), and plan: [B] (first part, parts) for those who join them.
 template <int KV, int D, bool BF16, int NT>
 __global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS)
-kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
+kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, int room) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
@@ -134,20 +171,25 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
     __shared__ int s_heads;
     __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, t4 = lane & 3;
-    const int split = blockIdx.x % n_splits, bg = blockIdx.x / n_splits, b = bg / a.Hk, g = bg % a.Hk;
+    const int g = blockIdx.x % a.Hk;
     grid_dependents_start_if_small();
     grid_dependency_wait();
+    RowsShare share = {(int)blockIdx.x / a.Hk, 0, 1, 0};
+    int chunk = 0x7fffffff / kKeys;
+    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room, chunk);   // (every warp for itself)
+    if (share.b < 0) return;
+    const int b = share.b;
     if (warp == 0) {
-        const int n = kv_group_heads(a, b, g, g == 0 && split == 0 && blockIdx.y == 0, s_head, s_pos);
+        const int n = kv_group_heads(a, b, g, g == 0 && share.split == 0 && blockIdx.y == 0, s_head, s_pos);
         if (lane == 0) s_heads = n;
+        if (room > 0 && lane == 0 && share.split == 0 && g == 0 && blockIdx.y == 0) plan[b] = make_int2(share.first, share.n);
     }
     const int len = kv_length(a, b);
     const uint32_t mask = a.masks ? a.masks[b] : 0u;
     __syncthreads();
     const int rows = s_heads * a.Tq;
     const int tiles = (len + kKeys - 1) / kKeys;
-    const int per_split = ((tiles + n_splits - 1) / n_splits + kWarps - 1) / kWarps * kWarps;
-    const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles);
+    const int t0 = min(share.split * chunk, tiles), t1 = min(t0 + chunk, tiles);
     const uint32_t ring = ptx::smem_u32(smem) + warp * C::STAGES * C::STAGE;
     RowsMeta* meta = s_meta[warp];
     const char *kbase, *vbase;
@@ -174,75 +216,74 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
         constexpr int RPI = 32 / C::CHUNKS;
         const int my_row = lane / C::CHUNKS, my_chunk = lane % C::CHUNKS;
         const int my_dst = my_row * C::ROW + ((my_chunk ^ bank_shift<C::CHUNKS>(my_row)) << 4);
+        // K's and V's copies of a tile are two groups: the slot of K is free, and filled again, half a tile before that of V
         int next = t0 + warp, next_slot = 0, ahead = look_ahead(next);
-        auto issue = [&]() {
+        unsigned next_vis = 0;
+        long long off[2] = {0, 0};                   // where this lane's first pieces of the tile lie, of its first 16 keys and of the others
+        auto issue = [&](bool is_v) {
             if (next < t1) {
-                const uint32_t dst = ring + next_slot * C::STAGE;
-                RowsMeta* mt = meta + next_slot;
+                const uint32_t dst = ring + next_slot * C::STAGE + (is_v ? kKeys * C::ROW : 0);
                 const int n0 = next * kKeys;
-                bool ok = n0 + lane < len;
-                if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
-                else {
-                    const bool good = (unsigned)ahead < (unsigned)a.n_pages;
-                    if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
-                    ok = ok && good;
-                }
-                const unsigned vis = __ballot_sync(0xffffffffu, ok);
-                if (lane == 0) mt->vis = vis;
-                if (vis != 0) {
-                    const char *kp[2], *vp[2];       // this lane's first piece among the first 16 keys, and among the others
-                    if constexpr (DENSE) {
-                        kp[0] = kbase + ((long long)(n0 + my_row) * a.ks[2] + my_chunk * 8) * 2;
-                        vp[0] = vbase + ((long long)(n0 + my_row) * a.vs[2] + my_chunk * 8) * 2;
-                    } else {
+                if (!is_v) {
+                    RowsMeta* mt = meta + next_slot;
+                    bool ok = n0 + lane < len;
+                    if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
+                    else {
+                        const bool good = (unsigned)ahead < (unsigned)a.n_pages;
+                        if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                        ok = ok && good;
+                    }
+                    next_vis = __ballot_sync(0xffffffffu, ok);
+                    if (lane == 0) mt->vis = next_vis;
+                    if constexpr (!DENSE) {
                         if ((lane & 15) == 0 && ok) {
                             const size_t ph = (size_t)ahead * a.Hk + g;
                             cp_async_4(ptx::smem_u32(&mt->ks[lane >> 4]), a.k_scales + ph);
                             cp_async_4(ptx::smem_u32(&mt->vs[lane >> 4]), a.v_scales + ph);
                         }
                         const int id0 = __shfl_sync(0xffffffffu, ahead, 0), id1 = __shfl_sync(0xffffffffu, ahead, 16);
-                        const size_t o0 = ((((size_t)id0 * a.Hk + g) << page_shift) + (n0 & (a.page - 1))) * D + lane * 16;
-                        const size_t o1 = ((((size_t)id1 * a.Hk + g) << page_shift) + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
-                        kp[0] = kbase + o0; vp[0] = vbase + o0;
-                        kp[1] = kbase + o1; vp[1] = vbase + o1;
+                        off[0] = ((((long long)id0 * a.Hk + g) << page_shift) + (n0 & (a.page - 1))) * D + lane * 16;
+                        off[1] = ((((long long)id1 * a.Hk + g) << page_shift) + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
                     }
-                    auto piece = [&](int i, const char*& ks, const char*& vs) {
-                        if constexpr (DENSE) {
-                            ks = kp[0] + (long long)(i * RPI) * a.ks[2] * 2;
-                            vs = vp[0] + (long long)(i * RPI) * a.vs[2] * 2;
-                        } else {
+                }
+                if (next_vis != 0) {
+                    const char* base = is_v ? vbase : kbase;
+                    const long long step = DENSE ? (is_v ? a.vs[2] : a.ks[2]) * 2 : 0;
+                    const char* first = DENSE ? base + (n0 + my_row) * step + my_chunk * 16 : base;
+                    auto piece = [&](int i, const char*& src) {
+                        if constexpr (DENSE) src = first + i * RPI * step;
+                        else {
                             const int h = C::CHUNKS == 1 ? (lane >> 4) : i >= C::CHUNKS / 2, j = C::CHUNKS == 1 ? 0 : i - h * (C::CHUNKS / 2);
-                            ks = (h ? kp[1] : kp[0]) + j * 512;
-                            vs = (h ? vp[1] : vp[0]) + j * 512;
+                            src = base + (h ? off[1] : off[0]) + j * 512;
                         }
                         return dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
                     };
-                    const char *ks, *vs;
-                    if (vis == 0xffffffffu) {
+                    const char* src;
+                    if (next_vis == 0xffffffffu) {
 #pragma unroll
                         for (int i = 0; i < C::CHUNKS; ++i) {
-                            const uint32_t at = piece(i, ks, vs);
-                            cp_async_16_full(at, ks);
-                            cp_async_16_full(at + kKeys * C::ROW, vs);
+                            const uint32_t at = piece(i, src);
+                            cp_async_16_full(at, src);
                         }
                     } else {
 #pragma unroll 1
                         for (int i = 0; i < C::CHUNKS; ++i) {
-                            const uint32_t at = piece(i, ks, vs);
-                            const bool yes = (vis >> (i * RPI + my_row)) & 1u;
-                            cp_async_16_or_zero(at, yes ? ks : kbase, yes);
-                            cp_async_16_or_zero(at + kKeys * C::ROW, yes ? vs : vbase, yes);
+                            const uint32_t at = piece(i, src);
+                            const bool yes = (next_vis >> (i * RPI + my_row)) & 1u;
+                            cp_async_16_or_zero(at, yes ? src : base, yes);
                         }
                     }
                 }
-                next += kWarps;
-                next_slot = next_slot + 1 == C::STAGES ? 0 : next_slot + 1;
-                ahead = look_ahead(next);
+                if (is_v) {
+                    next += kWarps;
+                    next_slot = next_slot + 1 == C::STAGES ? 0 : next_slot + 1;
+                    ahead = look_ahead(next);
+                }
             }
             ptx::cp_async_commit();
         };
-#pragma unroll
-        for (int s = 0; s < C::STAGES - 1; ++s) issue();
+#pragma unroll 1
+        for (int s = 0; s < C::STAGES; ++s) { issue(false); issue(true); }
 
         // -------------------------------------------------------------------- rows of Q as MMA operands: lane (gq, t4) has row gq of every eight
         uint32_t qf[NT][KSTEPS][2];
@@ -324,16 +365,16 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
         // -------------------------------------------------------------------- tiles of 32 keys
         int slot = 0;
         for (int tile = t0 + warp; tile < t1; tile += kWarps) {
-            issue();
-            ptx::cp_async_wait_group<C::STAGES - 1>();
+            ptx::cp_async_wait_group<2 * C::STAGES - 1>();
             __syncwarp();
             const int n0 = tile * kKeys;
             const uint32_t kt = ring + slot * C::STAGE, vt = kt + kKeys * C::ROW;
             const unsigned vis = meta[slot].vis;
+            const float vscale[2] = {DENSE ? 1.0f : meta[slot].vs[0], DENSE ? 1.0f : meta[slot].vs[1]};
+            const bool full = vis == 0xffffffffu && n0 + kKeys <= all_see;
+            float s[2][NT][4];
             if (vis != 0) {
-                const bool full = vis == 0xffffffffu && n0 + kKeys <= all_see;
                 // ------ scores: element (key mt * 16 + gq + 8 * (x >> 1), row nt * 8 + 2 t4 + (x & 1))
-                float s[2][NT][4];
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
@@ -369,6 +410,10 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                         for (int x = 0; x < 4; ++x) s[mt][nt][x] *= x & 1 ? c1 : c0;
                     }
                 }
+            }
+            __syncwarp();
+            issue(false);
+            if (vis != 0) {
                 if (!full) {
 #pragma unroll
                     for (int mt = 0; mt < 2; ++mt)
@@ -421,6 +466,8 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                             l[nt][x & 1] += s[mt][nt][x];
                         }
                 }
+                ptx::cp_async_wait_group<2 * C::STAGES - 1>();
+                __syncwarp();
                 // ------ values, 16 keys at a time: column gq * (D / 8) + 2 j is row gq of the MMA's tile j, the next column its row gq + 8
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
@@ -428,7 +475,7 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                         // The page's scale multiplies the weights, as a ratio to vref; where it is far from that, O changes its unit.
                         // (A page 2^64 times smaller leaves it: its values are nothing beside what O may hold.)
                         if (((vis >> (kk * 16)) & 0xffffu) == 0) continue;
-                        const float vs = meta[slot].vs[kk];
+                        const float vs = vscale[kk];
                         float ratio = vs * inv_vref;
                         if (!(fabsf(ratio) >= 0.0625f && fabsf(ratio) <= 16.0f)) {
                             if (!(fabsf(vs) <= 3.4028234e38f)) ratio = __int_as_float(0x7fc00000);
@@ -517,8 +564,9 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                     }
                 }
             }
-            slot = slot + 1 == C::STAGES ? 0 : slot + 1;
             __syncwarp();
+            issue(true);
+            slot = slot + 1 == C::STAGES ? 0 : slot + 1;
         }
         ptx::cp_async_wait_all();
         // -------------------------------------------------------------------- the four warps' parts
@@ -555,12 +603,12 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                 x += v.x * f;
                 y += v.y * f;
             }
-            const size_t out = ((size_t)b * a.k_h + s_pos[row / a.Tq]) * a.Tq + row % a.Tq;
-            if (n_splits == 1) {
+            const size_t in = (size_t)s_pos[row / a.Tq] * a.Tq + row % a.Tq, out = (size_t)b * a.k_h * a.Tq + in;
+            if (share.n == 1) {
                 const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
                 reinterpret_cast<uint32_t*>(a.O)[(out * D + c) / 2] = pack2<BF16>(sum == 0.0f ? 0.0f : x * inv, sum == 0.0f ? 0.0f : y * inv);
             } else {
-                const size_t at = (size_t)split * a.B * a.k_h * a.Tq + out;
+                const size_t at = (size_t)(share.first + share.split) * a.k_h * a.Tq + in;
                 *reinterpret_cast<float2*>(part + at * D + c) = make_float2(x, y);
                 if (c == 0) ml[at] = make_float2(top, sum);
             }
@@ -579,29 +627,24 @@ long long rows_tiles(const KvAttendArgs& a) {
     const long long n = ((long long)heads * a.Tq + tile - 1) / tile;
     return n < 64 ? n : 64;
 }
-// Blocks along the keys: as many as one wave holds, each with a tile for every warp at least.
-int rows_splits(const KvAttendArgs& a) {
-    // blocks that the GPU holds at a time (RowsCfg::BLOCKS)
-    const long long slots = (a.format == 0 && a.d == 128 ? 1 : 3) * kSmCount;
-    const long long blocks = (long long)a.B * a.Hk * rows_tiles(a);
-    const long long most = ((long long)a.Tk + kWarps * kKeys - 1) / (kWarps * kKeys);
-    if (blocks == 0) return 1;
-    long long n = slots / blocks;
-    if (n > most) n = most;
-    if (n > 128) n = 128;
-    return n < 1 ? 1 : (int)n;
+// Blocks that one wave holds for every row tile (RowsCfg::BLOCKS an SM); 0: the groups alone fill it, and no axis is split.
+int rows_wave(const KvAttendArgs& a) {
+    const long long slots = (a.format == 0 && a.d == 128 ? 1 : 3) * kSmCount, wave = rows_tiles(a) > 0 ? slots / rows_tiles(a) : 0;
+    return a.B < wave / a.Hk && a.Tk > kWarps * kKeys ? (int)wave : 0;
 }
 
 template <int KV, int D, bool BF16, int NT>
 int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     using C = RowsCfg<KV, D>;
-    const int n_splits = rows_splits(a);
-    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
+    const int wave = rows_wave(a), room = wave / a.Hk - a.B;      // parts beside the first of every sample
+    const size_t rows = (size_t)a.k_h * a.Tq;
     float* part = nullptr;
     float2* ml = nullptr;
-    if (n_splits > 1) {
-        part = ws.take<float>(n_splits * rows * D);
-        ml = ws.take<float2>(n_splits * rows);
+    int2* plan = nullptr;
+    if (wave > 0) {
+        part = ws.take<float>(wave / a.Hk * rows * D);
+        ml = ws.take<float2>(wave / a.Hk * rows);
+        plan = ws.take<int2>(a.B);
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
     auto k = kv_rows_kernel<KV, D, BF16, NT>;
@@ -609,9 +652,10 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
-        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)rows_tiles(a)), dim3(kWarps * 32), C::SMEM, st, a, part, ml, n_splits));
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kWarps * 32), C::SMEM, st, a, part, ml,
+                                       plan, wave > 0 ? room : 0));
     }
-    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
+    return wave > 0 ? launch_kv_combine(ctx, a, part, ml, plan, 0, st) : SENTRY_OK;
 }
 
 template <int KV, int D, bool BF16>
@@ -632,10 +676,10 @@ int launch_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t s
 }  // namespace
 
 size_t kv_rows_ws_bytes(const KvAttendArgs& a) {
-    const int n = rows_splits(a);
-    if (n <= 1) return 0;
-    const size_t rows = (size_t)a.B * a.k_h * a.Tq;
-    return align_up(n * rows * a.d * sizeof(float), 256) + n * rows * sizeof(float2) + 512;
+    const int wave = rows_wave(a);
+    if (wave == 0) return 0;
+    const size_t parts = wave / a.Hk, rows = (size_t)a.k_h * a.Tq;
+    return align_up(parts * rows * a.d * sizeof(float), 256) + align_up(parts * rows * sizeof(float2), 256) + a.B * sizeof(int2) + 512;
 }
 
 int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {

@@ -307,8 +307,8 @@ kv_tc_kernel(const __grid_constant__ TcMaps maps, const KvAttendArgs a, const in
                 ptx::tc_fence_after_sync();
                 if (ok) {
                     const bool in = row < rows;
-                    const size_t out = in ? ((size_t)b * a.k_h + misc->pos[row / a.Tq]) * a.Tq + row % a.Tq : 0;
-                    const size_t pat = (size_t)split * a.B * a.k_h * a.Tq + out;
+                    const size_t each = (size_t)a.k_h * a.Tq, within = in ? (size_t)misc->pos[row / a.Tq] * a.Tq + row % a.Tq : 0;
+                    const size_t out = b * each + within, pat = ((size_t)b * n_splits + split) * each + within;
                     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                     if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * c - kShift, l) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
@@ -444,7 +444,7 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
         SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(kTcThreads), TcCfg<D>::SMEM, st, maps, a,
                                        (const int32_t*)list, (const int32_t*)counts, part, ml, n_splits));
     }
-    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
+    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, nullptr, n_splits, st) : SENTRY_OK;
 }
 
 template <bool BF16>

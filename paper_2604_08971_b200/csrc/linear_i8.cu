@@ -15,7 +15,7 @@ namespace {
 // ------------------------------------------------------------------------------------------------ quantise rows
 // WARPS warps share a row (1: eight rows a block; 8: one row a block).  Up to HELD pieces of 16 bytes a lane stay in registers between the
 // two steps; what a longer row has beyond them is read a second time.  Bound by the bytes, as long as a value costs few instructions:
-// the maximum runs on pairs of magnitude bits, and the quotient is rounded by an addition unless it lies next to a half (codes_i8).
+// the maximum runs on pairs of magnitude bits, and the quotient is rounded by an addition, two at a time (codes_i8).
 template <typename T, int WARPS, int HELD>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ X, int8_t* __restrict__ codes, float* __restrict__ scales,
                                                             int M, int K) {
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
     }
     const float most = magnitude<T>(bits);
     const float s = isnan(most) ? most : scale_i8(most);
-    const float inv = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
+    const float inv = s > 0.0f ? reciprocal_i8(s, most) : 0.0f;
     if (at == 0) scales[row] = s;
     int8_t* dst = codes + row * K;
     auto put = [&](const uint4& v, int p) {

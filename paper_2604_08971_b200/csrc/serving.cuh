@@ -37,7 +37,7 @@ size_t kv_rows_ws_bytes(const KvAttendArgs& a);
 bool kv_tc_takes(const KvAttendArgs& a);                                                   // 16-bit dense, many rows
 size_t kv_tc_ws_bytes(const KvAttendArgs& a);
 int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);
-int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, int n_splits, cudaStream_t st);
+int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, const int2* plan, int n_splits, cudaStream_t st);
 int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);   // 16-bit rows, few of them
 
 struct AppendArgs {
@@ -74,33 +74,57 @@ __device__ __forceinline__ int round_quotient_i8(float x, float s, float inv) {
     else if (e2 < -s || (e2 == -s && odd)) r -= 1.0f;
     return (int)fminf(fmaxf(r, -127.0f), 127.0f);
 }
-// N values over s (positive): codes as words.  Adding 1.5 * 2^23 rounds x * inv to an integer r and leaves it in the low bits; that is one
-// off where the quotient lies next to a half (which is common: two bf16 numbers' quotient is one of few fractions).  The remainder
-// x - r s is exact, and twice it against s says so; an exact half, which has to go to the even side, is left to round_quotient_i8.
+// N values over s (positive): codes as words.  Adding 1.5 * 2^23 rounds x * inv to an integer r and leaves it in the low bits, two values at a
+// time.  The remainder x - r s is exact; where it is half of s or more, r may be the wrong neighbour, or the quotient an exact half, which
+// has to go to the even side: round_quotient_i8 decides.  That would be common (two bf16 numbers' quotient is one of few fractions, a
+// half often), but for reciprocal_i8.
 __device__ __forceinline__ uint32_t pack_low_bytes(float a, float b, float c, float d) {
     return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
+// 1 / s, moved by 2^-22 of itself to the side on which s was rounded from top / 127: a quotient that would be a half but for that
+// rounding then falls where the exact one does.
+__device__ __forceinline__ float reciprocal_i8(float s, float top) {
+    const float inv = __fdiv_rn(1.0f, s), r = fmaf(-127.0f, s, top);
+    return r < 0.0f ? inv * (1.0f - 2.38418579e-7f) : r > 0.0f ? inv * (1.0f + 2.38418579e-7f) : inv;
+}
+__device__ __forceinline__ uint64_t pair_f32(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(uint64_t p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
 }
 template <int N>
 __device__ __forceinline__ void codes_i8(const float (&x)[N], float s, float inv, uint32_t (&w)[N / 4]) {
     constexpr float kMagic = 12582912.0f;
-    float y[N];
-    bool half = false;
+    const uint64_t magic = pair_f32(kMagic, kMagic), minus = pair_f32(-1.0f, -1.0f), inv2 = pair_f32(inv, inv), s2 = pair_f32(s, s);
+    float y[N], far = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        y[i] = fmaf(x[i], inv, kMagic);
-        const float e = fmaf(kMagic - y[i], s, x[i]), d = fmaf(2.0f, fabsf(e), -s);
-        if (d > 0.0f) y[i] += copysignf(1.0f, e);
-        half = half || d == 0.0f;
+    for (int i = 0; i < N; i += 2) {
+        const uint64_t xx = pair_f32(x[i], x[i + 1]), yy = fma_pair(xx, inv2, magic);
+        const float2 e = pair_of(fma_pair(fma_pair(yy, minus, magic), s2, xx)), v = pair_of(yy);
+        far = fmaxf(far, fmaxf(fabsf(e.x), fabsf(e.y)));
+        y[i] = v.x;
+        y[i + 1] = v.y;
     }
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) w[i] = pack_low_bytes(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-    if (half) {
+    if (far + far >= s) {
+        const float exact_inv = __fdiv_rn(1.0f, s);
 #pragma unroll 1
         for (int i = 0; i < N; ++i) {
             float v = x[0];
 #pragma unroll
             for (int j = 1; j < N; ++j) v = j == i ? x[j] : v;       // (no indexed registers)
-            const uint32_t c = (uint32_t)(round_quotient_i8(v, s, inv) & 255) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
+            const uint32_t c = (uint32_t)(round_quotient_i8(v, s, exact_inv) & 255) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
 #pragma unroll
             for (int j = 0; j < N / 4; ++j) w[j] = j == i / 4 ? (w[j] & keep) | c : w[j];
         }
