@@ -51,20 +51,24 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
     const float inv = s > 0.0f ? reciprocal_i8(s, most) : 0.0f;
     if (at == 0) scales[row] = s;
     int8_t* dst = codes + row * K;
-    auto put = [&](const uint4& v, int p) {
-        float f[N];
-        uint32_t w[N / 4] = {};
-        Vec16<T>::get(v, f);
-        if (s > 0.0f) codes_i8<N>(f, s, inv, w);
-        if constexpr (N == 8) *reinterpret_cast<uint2*>(dst + (size_t)p * 8) = make_uint2(w[0], w[1]);
-        else *reinterpret_cast<uint32_t*>(dst + (size_t)p * 4) = w[0];
-    };
+    auto put_all = [&](auto check) {
+        auto put = [&](const uint4& v, int p) {
+            float f[N];
+            uint32_t w[N / 4] = {};
+            Vec16<T>::get(v, f);
+            if (s > 0.0f) codes_i8<decltype(check)::value, N>(f, s, inv, w);
+            if constexpr (N == 8) *reinterpret_cast<uint2*>(dst + (size_t)p * 8) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(dst + (size_t)p * 4) = w[0];
+        };
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const int p = at + i * LANES;
-        if (p < pieces) put(held[i], p);
-    }
-    for (int p = at + HELD * LANES; p < pieces; p += LANES) put(src[p], p);
+        for (int i = 0; i < HELD; ++i) {
+            const int p = at + i * LANES;
+            if (p < pieces) put(held[i], p);
+        }
+        for (int p = at + HELD * LANES; p < pieces; p += LANES) put(src[p], p);
+    };
+    if (sure_i8<T>(s, most)) put_all(std::false_type());
+    else put_all(std::true_type());
 }
 
 template <typename T>
@@ -309,17 +313,32 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
         bool ok = true;
         uint32_t n = 0;
         const bool whole = N % PER == 0;                                      // rows of Y start on 16 bytes
+        // scales and biases of the next tile, asked for while this one is worked on
+        constexpr int AHEAD = STEPS * COLS / 32;
+        float next_scale[AHEAD], next_bias[AHEAD], next_sx = 0.0f;
+        auto ask = [&](long long tile) {
+            const int m = (int)(tile / n_tiles) * 128 * P + rank * 128 + quarter * 32 + lane, n0 = (int)(tile % n_tiles) * BN;
+            next_sx = tile < tiles && m < M ? xs[m] : 0.0f;
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) {
+                const int e = x * 32 + lane, col = n0 + (e / COLS * 2 + half) * COLS + e % COLS;
+                const bool in = tile < tiles && col < N;
+                next_scale[x] = in ? ws[col] : 0.0f;
+                next_bias[x] = in && bias != nullptr ? bias[col] : 0.0f;
+            }
+        };
+        ask(tile0);
         for (long long tile = tile0; tile < tiles && ok; tile += tile_step, ++n) {
             const uint32_t buf = n & 1, acc = tmem + buf * BN + ((uint32_t)(quarter * 32) << 16);
             const int m0 = (int)(tile / n_tiles) * 128 * P + rank * 128 + quarter * 32, n0 = (int)(tile % n_tiles) * BN;
-            const float sx = m0 + lane < M ? xs[m0 + lane] : 0.0f;
+            const float sx = next_sx;
 #pragma unroll
-            for (int e = lane; e < STEPS * COLS; e += 32) {
-                const int col = n0 + (e / COLS * 2 + half) * COLS + e % COLS;
-                s_scale[e] = col < N ? ws[col] : 0.0f;
-                s_bias[e] = bias != nullptr && col < N ? bias[col] : 0.0f;
+            for (int x = 0; x < AHEAD; ++x) {
+                s_scale[x * 32 + lane] = next_scale[x];
+                s_bias[x * 32 + lane] = next_bias[x];
             }
             __syncwarp();
+            ask(tile + tile_step);
             ok = warp_wait(&misc->acc_full[buf], (n >> 1) & 1, abort_flag);
             if (!ok) break;
             ptx::tc_fence_after_sync();
@@ -333,6 +352,7 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
                 ptx::tmem_ld_wait();
                 const float4* sc4 = reinterpret_cast<const float4*>(s_scale + step * COLS);
                 const float4* bi4 = reinterpret_cast<const float4*>(s_bias + step * COLS);
+                const uint64_t sx2 = pair_f32(sx, sx);
 #pragma unroll
                 for (int i = 0; i < COLS; i += PER) {
                     float y[PER];
@@ -340,10 +360,13 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
                     for (int x = 0; x < PER; x += 4) {
                         const float4 f = sc4[(i + x) / 4], c = bi4[(i + x) / 4];
                         const uint32_t* q = &r[(i + x) / 32][(i + x) % 32];
-                        y[x] = fmaf((float)(int32_t)q[0] * sx, f.x, c.x);
-                        y[x + 1] = fmaf((float)(int32_t)q[1] * sx, f.y, c.y);
-                        y[x + 2] = fmaf((float)(int32_t)q[2] * sx, f.z, c.z);
-                        y[x + 3] = fmaf((float)(int32_t)q[3] * sx, f.w, c.w);
+                        const uint64_t lo = mul_pair(pair_f32((float)(int32_t)q[0], (float)(int32_t)q[1]), sx2);
+                        const uint64_t hi = mul_pair(pair_f32((float)(int32_t)q[2], (float)(int32_t)q[3]), sx2);
+                        const float2 u = pair_of(fma_pair(lo, pair_f32(f.x, f.y), pair_f32(c.x, c.y))), v = pair_of(fma_pair(hi, pair_f32(f.z, f.w), pair_f32(c.z, c.w)));
+                        y[x] = u.x;
+                        y[x + 1] = u.y;
+                        y[x + 2] = v.x;
+                        y[x + 3] = v.y;
                     }
                     uint32_t w[4];
                     if constexpr (sizeof(T) == 4) {

@@ -63,21 +63,15 @@ struct LinearArgs {
 int launch_linear_i8(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st);
 
 #ifdef __CUDACC__
-// x / s to the nearest integer, ties to even, of the exact quotient; |x| <= 127 s (1 + 2^-22), s >= 2^-126, inv = 1 / s rounded.
-// The product with the rounded reciprocal is at most one off; x - r s is exact (a multiple of the smaller operand's last place, below
-// s in size), and twice it against s says which neighbour is nearer.
-__device__ __forceinline__ int round_quotient_i8(float x, float s, float inv) {
-    float r = rintf(x * inv);
-    const float e2 = 2.0f * fmaf(-r, s, x);
-    const bool odd = ((int)r) & 1;
-    if (e2 > s || (e2 == s && odd)) r += 1.0f;
-    else if (e2 < -s || (e2 == -s && odd)) r -= 1.0f;
-    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
-}
-// N values over s (positive): codes as words.  Adding 1.5 * 2^23 rounds x * inv to an integer r and leaves it in the low bits, two values at a
-// time.  The remainder x - r s is exact; where it is half of s or more, r may be the wrong neighbour, or the quotient an exact half, which
-// has to go to the even side: round_quotient_i8 decides.  That would be common (two bf16 numbers' quotient is one of few fractions, a
-// half often), but for reciprocal_i8.
+// N values over s (positive): codes as words.  Adding 1.5 * 2^23 rounds x * inv to an integer and leaves it in the low bits, two values at a
+// time; |x| <= 127 s (1 + 2^-22), s >= 2^-126.  The product with the rounded reciprocal is at most one off.  With CHECK the remainder
+// x - r s (exact: a multiple of the smaller operand's last place, below s in size) says which neighbour is nearer, and an exact half goes
+// to the even one.
+// Without CHECK that cannot be (sure_i8).  Let x = m 2^i and top = t 2^j with whole m, t <= 2047, as 16-bit numbers are, s = top / 127 up to
+// two roundings, and inv as reciprocal_i8 gives it: x * inv is 127 x / top = 127 m / (t 2^k) up to 2^-21 of itself (s 2^-23, 1 / s 2^-24, the
+// move 2^-22 and its rounding 2^-24).  That fraction is a half of an odd number or at least 1 / (t 2^(k+1)) away from one, and 2^-21 of it
+// is less, since 127 m < 2^20.  Where it is a half, x / s lies on the side to which s was rounded, and inv was moved there by more than its
+// error; only where s was not rounded at all is it a half indeed.
 __device__ __forceinline__ uint32_t pack_low_bytes(float a, float b, float c, float d) {
     return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
@@ -86,6 +80,11 @@ __device__ __forceinline__ uint32_t pack_low_bytes(float a, float b, float c, fl
 __device__ __forceinline__ float reciprocal_i8(float s, float top) {
     const float inv = __fdiv_rn(1.0f, s), r = fmaf(-127.0f, s, top);
     return r < 0.0f ? inv * (1.0f - 2.38418579e-7f) : r > 0.0f ? inv * (1.0f + 2.38418579e-7f) : inv;
+}
+// Whether codes_i8 needs no check: values of a 16-bit type under the scale of the largest of them.
+template <typename T>
+__device__ __forceinline__ bool sure_i8(float s, float top) {
+    return sizeof(T) == 2 && s > 1.17549435e-38f && fmaf(-127.0f, s, top) != 0.0f;
 }
 __device__ __forceinline__ uint64_t pair_f32(float lo, float hi) {
     uint64_t r;
@@ -102,33 +101,31 @@ __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-template <int N>
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+template <bool CHECK, int N>
 __device__ __forceinline__ void codes_i8(const float (&x)[N], float s, float inv, uint32_t (&w)[N / 4]) {
     constexpr float kMagic = 12582912.0f;
-    const uint64_t magic = pair_f32(kMagic, kMagic), minus = pair_f32(-1.0f, -1.0f), inv2 = pair_f32(inv, inv), s2 = pair_f32(s, s);
-    float y[N], far = 0.0f;
+    const uint64_t magic = pair_f32(kMagic, kMagic), inv2 = pair_f32(inv, inv);
+    float y[N];
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-        const uint64_t xx = pair_f32(x[i], x[i + 1]), yy = fma_pair(xx, inv2, magic);
-        const float2 e = pair_of(fma_pair(fma_pair(yy, minus, magic), s2, xx)), v = pair_of(yy);
-        far = fmaxf(far, fmaxf(fabsf(e.x), fabsf(e.y)));
+        const float2 v = pair_of(fma_pair(pair_f32(x[i], x[i + 1]), inv2, magic));
         y[i] = v.x;
         y[i + 1] = v.y;
     }
+    if constexpr (CHECK) {
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) w[i] = pack_low_bytes(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-    if (far + far >= s) {
-        const float exact_inv = __fdiv_rn(1.0f, s);
-#pragma unroll 1
         for (int i = 0; i < N; ++i) {
-            float v = x[0];
-#pragma unroll
-            for (int j = 1; j < N; ++j) v = j == i ? x[j] : v;       // (no indexed registers)
-            const uint32_t c = (uint32_t)(round_quotient_i8(v, s, exact_inv) & 255) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
-#pragma unroll
-            for (int j = 0; j < N / 4; ++j) w[j] = j == i / 4 ? (w[j] & keep) | c : w[j];
+            const float e = fmaf(kMagic - y[i], s, x[i]), d = fmaf(2.0f, fabsf(e), -s);
+            if (d > 0.0f || (d == 0.0f && (__float_as_uint(y[i]) & 1u))) y[i] += copysignf(1.0f, e);
         }
     }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = pack_low_bytes(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
 }
 // (the product with 1/127 rounded to fp32, not the quotient: what the header defines)
 __device__ __forceinline__ float scale_i8(float top) { return top > 0.0f ? fmaxf(__fmul_rn(top, 1.0f / 127.0f), 1.17549435e-38f) : 0.0f; }
@@ -165,11 +162,11 @@ template <> struct Vec16<__half> {
 template <typename T> struct AbsMax {
     uint32_t acc = 0;
     __device__ __forceinline__ void add(const uint4& v) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) acc = max(acc, w[i] & 0x7fffffffu);
-            else acc = __vmaxu2(acc, w[i] & 0x7fff7fffu);
+        if constexpr (sizeof(T) == 4) {
+            acc = max(acc, max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)));
+        } else {
+            acc = __vimax3_u16x2(acc, v.x & 0x7fff7fffu, v.y & 0x7fff7fffu);
+            acc = __vimax3_u16x2(acc, v.z & 0x7fff7fffu, v.w & 0x7fff7fffu);
         }
     }
     __device__ __forceinline__ uint32_t bits() const { return sizeof(T) == 4 ? acc : max(acc & 0xffffu, acc >> 16); }
