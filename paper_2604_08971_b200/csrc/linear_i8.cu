@@ -172,7 +172,9 @@ __host__ __device__ constexpr uint32_t umma_idesc_i8(int M, int N) {
 
 // A tile: 128 P tokens x BN channels, K in steps of 128 bytes; a pair's CTAs have 128 tokens and half of the channels' weights each, so that
 // a tile costs the L2 and shared memory two thirds of what two single CTAs' would.  Two accumulators in tensor memory: the eight
-// epilogue warps scale and store one while the other is summed.
+// epilogue warps scale one and store it, by TMA, while the other is summed.
+// Tried without gain at 65536 x 1024 x 2048 (108 us): the accumulator handed over before it is scaled (115), sixteen epilogue warps
+// (114), six stages and stores of 32 bytes a row (125), a pair's weights kept in shared memory with three stages of X (141).
 constexpr int kLinThreads = 384, kLinEpiWarp0 = 4, kLinEpiWarps = 8;
 
 template <int P, int BN>
@@ -181,8 +183,8 @@ struct LinCfg {
     static constexpr int STAGE = (128 + B_ROWS) * 128;
     static constexpr int STAGES = 163840 / STAGE > 8 ? 8 : 163840 / STAGE;
     static constexpr int TMEM = BN <= 64 ? 128 : BN <= 128 ? 256 : 512;
-    static constexpr int EPI = 4096 + (BN < 128 ? 128 : BN) * 4;                // a warp's 32 rows of 128 bytes; scales and biases of its half of the columns
-    static constexpr int SMEM = STAGES * STAGE + kLinEpiWarps * EPI + 1024;
+    static constexpr int EPI = 4096, SCALES = (BN < 128 ? 128 : BN) * 4;   // a warp's 32 rows of 128 bytes; scales and biases of its columns
+    static constexpr int SMEM = STAGES * STAGE + kLinEpiWarps * (EPI + SCALES) + 1024;
 };
 struct LinMisc {
     uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
@@ -202,9 +204,28 @@ bool make_map_i8(CUtensorMap* tm, const void* ptr, uint64_t rows, uint64_t K, ui
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Y [M, N] row-major -> boxes of 32 rows x 128 bytes, 128-byte swizzle; what lies outside is not written
+template <typename T>
+bool make_map_out(CUtensorMap* tm, const void* ptr, uint64_t M, uint64_t N) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (fn == nullptr) return false;
+    cuuint64_t dims[2] = {N, M};
+    cuuint64_t strides[1] = {N * sizeof(T)};
+    cuuint32_t box[2] = {128 / (cuuint32_t)sizeof(T), 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(tm, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : std::is_same_v<T, __half> ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+              const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+__device__ __forceinline__ void tma_store_2d(const void* tmap, int x, int y, uint32_t smem) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(smem)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
 template <typename T, int P, int BN>
 __global__ void __launch_bounds__(kLinThreads, 1)
-linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const float* __restrict__ xs,
+linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const float* __restrict__ xs,
                     const float* __restrict__ ws, const float* __restrict__ bias, T* __restrict__ Y, int M, int K, int N, unsigned int* status) {
     using C = LinCfg<P, BN>;
     extern __shared__ uint8_t smem_raw[];
@@ -308,7 +329,8 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
         const int quarter = warp & 3, half = (warp - kLinEpiWarp0) >> 2;
         const uint32_t own = C::STAGES * C::STAGE + (base - raw_addr) + (warp - kLinEpiWarp0) * C::EPI;
         const uint32_t stg = raw_addr + own;
-        float* s_scale = reinterpret_cast<float*>(smem_raw + own + 4096);     // [STEPS * COLS] scales, then biases
+        float* s_scale = reinterpret_cast<float*>(smem_raw + C::STAGES * C::STAGE + (base - raw_addr) + kLinEpiWarps * C::EPI + (warp - kLinEpiWarp0) * C::SCALES);
+        // ([STEPS * COLS] scales, then biases)
         float* s_bias = s_scale + STEPS * COLS;
         bool ok = true;
         uint32_t n = 0;
@@ -350,6 +372,10 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
 #pragma unroll
                 for (int h = 0; h < COLS / 32; ++h) ptx::tmem_ld_32x32(acc + c0 + h * 32, r[h]);
                 ptx::tmem_ld_wait();
+                if (whole) {                       // the copy of the last 128 bytes has read them
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                }
                 const float4* sc4 = reinterpret_cast<const float4*>(s_scale + step * COLS);
                 const float4* bi4 = reinterpret_cast<const float4*>(s_bias + step * COLS);
                 const uint64_t sx2 = pair_f32(sx, sx);
@@ -383,15 +409,10 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
                                  "r"(w[3])
                                  : "memory");
                 }
+                if (whole) ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (whole) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = i * 4 + (lane >> 3), ch = lane & 7, col = n0 + c0 + ch * PER;
-                        uint4 v;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stg + row * 128 + ((ch ^ (row & 7)) << 4)));
-                        if (m0 + row < M && col < N) *reinterpret_cast<uint4*>(Y + (size_t)(m0 + row) * N + col) = v;
-                    }
+                    if (m0 < M && elect_one()) tma_store_2d(&tm_y, n0 + c0, m0, stg);
                 } else {
                     // rows that start anywhere: neighbouring lanes store neighbouring elements
                     const T* line = reinterpret_cast<const T*>(smem_raw + own);
@@ -416,6 +437,7 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
             }
         }
     }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // this thread's stores to Y
     if constexpr (P == 2) {
         __syncwarp();
         ptx::cluster_sync();                    // the pair's UMMAs read both CTAs' shared memory, its barriers hear from both
@@ -426,14 +448,15 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
 template <typename T, int P, int BN>
 int launch_tc(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
     using C = LinCfg<P, BN>;
-    CUtensorMap mx, mw;
+    CUtensorMap mx, mw, my = {};
     if (!make_map_i8(&mx, a.X, a.d.M, a.d.K, 128) || !make_map_i8(&mw, a.W, a.d.N, a.d.K, C::B_ROWS)) return SENTRY_ERR_CUDA;
+    if (a.d.N % (16 / (int)sizeof(T)) == 0 && !make_map_out<T>(&my, a.Y, a.d.M, a.d.N)) return SENTRY_ERR_CUDA;
     const long long tiles = (long long)((a.d.M + 128 * P - 1) / (128 * P)) * ((a.d.N + BN - 1) / BN), most = ctx->sm_count / P;
     auto k = linear_i8_tc_kernel<T, P, BN>;
     static std::atomic<unsigned long long> allowed{0};
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     LaunchScope ls(ctx, KS_LINEAR, st);
-    SENTRY_CUDA_TRY(launch_chained_clusters(P, k, dim3((unsigned)((tiles < most ? tiles : most) * P)), dim3(kLinThreads), C::SMEM, st, mx, mw, a.xs, a.ws, a.bias,
+    SENTRY_CUDA_TRY(launch_chained_clusters(P, k, dim3((unsigned)((tiles < most ? tiles : most) * P)), dim3(kLinThreads), C::SMEM, st, mx, mw, my, a.xs, a.ws, a.bias,
                                             (T*)a.Y, a.d.M, a.d.K, a.d.N, a.status));
     return SENTRY_OK;
 }
