@@ -27,10 +27,10 @@ struct RowsCfg {
     static constexpr int ROW = D * ESIZE;                    // bytes of a key
     static constexpr int CHUNKS = ROW / 16;
     static constexpr int STAGE = 2 * kKeys * ROW;            // K and V of a tile
-    // copies on the way: a tile a warp at least while it works on another, with three blocks on an SM (one for 16-bit rows of 128)
-    static constexpr int FIT = 65536 / (kWarps * STAGE);
-    static constexpr int STAGES = FIT < 2 ? 3 : FIT > 6 ? 6 : FIT;
-    static constexpr int BLOCKS = FIT < 2 ? 1 : 3;
+    // Two tiles of copies on the way for every warp at least, and as many blocks on an SM as that leaves room for.
+    static constexpr int FIT = 49152 / (kWarps * STAGE);
+    static constexpr int STAGES = FIT < 2 ? (STAGE > 8192 ? 3 : 2) : FIT > 4 ? 4 : FIT;
+    static constexpr int BLOCKS = STAGE > 8192 ? 1 : FIT < 2 ? 3 : 4;
     static constexpr int RING = kWarps * STAGES * STAGE;
     static constexpr int MERGE = kWarps * 16 * D * 4;
     static constexpr int SMEM = RING > MERGE ? RING : MERGE;
@@ -158,7 +158,7 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
 // room: 0: a block per group and row tile takes all of its keys.  Otherwise the keys are shared out (rows_share), part: [parts][k_h][Tq][D] sums,
 // ml: [parts][k_h][Tq] (maximum, total), and plan: [B] (first part, parts) for those who join them.
 template <int KV, int D, bool BF16, int NT>
-__global__ void __launch_bounds__(kWarps * 32, RowsCfg<KV, D>::BLOCKS)
+__global__ void __launch_bounds__(kWarps * 32, NT == 1 ? RowsCfg<KV, D>::BLOCKS : RowsCfg<KV, D>::BLOCKS < 3 ? 1 : 3)
 kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, int room) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
@@ -219,7 +219,19 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
         // K's and V's copies of a tile are two groups: the slot of K is free, and filled again, half a tile before that of V
         int next = t0 + warp, next_slot = 0, ahead = look_ahead(next);
         unsigned next_vis = 0;
-        long long off[2] = {0, 0};                   // where this lane's first pieces of the tile lie, of its first 16 keys and of the others
+        // this lane's first piece of the tile: of a dense tensor, or of a page and group (the pieces of a page's tile follow one another)
+        const char *k_first = kbase, *v_first = vbase;
+        long long k_step = 0, v_step = 0;
+        unsigned id[2] = {0, 0}, in_page = 0;                         // pages of the tile's first 16 keys and of the others; bytes into the first
+        if constexpr (DENSE) {
+            k_step = a.ks[2] * 2; v_step = a.vs[2] * 2;
+            k_first += my_row * k_step + my_chunk * 16;
+            v_first += my_row * v_step + my_chunk * 16;
+        } else {
+            k_first += (long long)(g << page_shift) * D + (C::CHUNKS > 1 ? lane : lane & 15) * 16;
+            v_first += (long long)(g << page_shift) * D + (C::CHUNKS > 1 ? lane : lane & 15) * 16;
+        }
+        const unsigned page_bytes = DENSE ? 0u : (unsigned)(a.Hk << page_shift) * D;    // of all groups: below 2^32
         auto issue = [&](bool is_v) {
             if (next < t1) {
                 const uint32_t dst = ring + next_slot * C::STAGE + (is_v ? kKeys * C::ROW : 0);
@@ -237,25 +249,29 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                     if (lane == 0) mt->vis = next_vis;
                     if constexpr (!DENSE) {
                         if ((lane & 15) == 0 && ok) {
-                            const size_t ph = (size_t)ahead * a.Hk + g;
+                            const size_t ph = (size_t)(unsigned)ahead * (unsigned)a.Hk + g;
                             cp_async_4(ptx::smem_u32(&mt->ks[lane >> 4]), a.k_scales + ph);
                             cp_async_4(ptx::smem_u32(&mt->vs[lane >> 4]), a.v_scales + ph);
                         }
-                        const int id0 = __shfl_sync(0xffffffffu, ahead, 0), id1 = __shfl_sync(0xffffffffu, ahead, 16);
-                        off[0] = ((((long long)id0 * a.Hk + g) << page_shift) + (n0 & (a.page - 1))) * D + lane * 16;
-                        off[1] = ((((long long)id1 * a.Hk + g) << page_shift) + ((n0 + 16) & (a.page - 1))) * D + (C::CHUNKS > 1 ? lane : lane - 16) * 16;
+                        id[0] = __shfl_sync(0xffffffffu, ahead, 0);
+                        id[1] = __shfl_sync(0xffffffffu, ahead, 16);
+                        in_page = (unsigned)(n0 & (a.page - 1)) * D;
                     }
                 }
                 if (next_vis != 0) {
                     const char* base = is_v ? vbase : kbase;
-                    const long long step = DENSE ? (is_v ? a.vs[2] : a.ks[2]) * 2 : 0;
-                    const char* first = DENSE ? base + (n0 + my_row) * step + my_chunk * 16 : base;
+                    const char* first = is_v ? v_first : k_first;
+                    const long long step = is_v ? v_step : k_step;
+                    const char *lo = first, *hi = first;
+                    if constexpr (DENSE) lo += n0 * step;
+                    else {
+                        lo += (unsigned long long)id[0] * page_bytes + in_page;
+                        hi = a.page == 16 ? first + (unsigned long long)id[1] * page_bytes : lo + 16 * D;
+                    }
                     auto piece = [&](int i, const char*& src) {
-                        if constexpr (DENSE) src = first + i * RPI * step;
-                        else {
-                            const int h = C::CHUNKS == 1 ? (lane >> 4) : i >= C::CHUNKS / 2, j = C::CHUNKS == 1 ? 0 : i - h * (C::CHUNKS / 2);
-                            src = base + (h ? off[1] : off[0]) + j * 512;
-                        }
+                        if constexpr (DENSE) src = lo + i * RPI * step;
+                        else if constexpr (C::CHUNKS == 1) src = lane < 16 ? lo : hi;
+                        else src = i < C::CHUNKS / 2 ? lo + i * 512 : hi + (i - C::CHUNKS / 2) * 512;
                         return dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
                     };
                     const char* src;
@@ -629,7 +645,8 @@ long long rows_tiles(const KvAttendArgs& a) {
 }
 // Blocks that one wave holds for every row tile (RowsCfg::BLOCKS an SM); 0: the groups alone fill it, and no axis is split.
 int rows_wave(const KvAttendArgs& a) {
-    const long long slots = (a.format == 0 && a.d == 128 ? 1 : 3) * kSmCount, wave = rows_tiles(a) > 0 ? slots / rows_tiles(a) : 0;
+    const int stage = 2 * kKeys * a.d * (a.format == 0 ? 2 : 1);
+    const long long slots = (stage > 8192 ? 1 : stage > 6144 || rows_tile(a) > 8 ? 3 : 4) * kSmCount, wave = rows_tiles(a) > 0 ? slots / rows_tiles(a) : 0;
     return a.B < wave / a.Hk && a.Tk > kWarps * kKeys ? (int)wave : 0;
 }
 
