@@ -39,7 +39,9 @@ int cross_args(const sentry_cross_desc* d, KvAttendArgs& a) {
     a.B = d->B; a.Tq = d->Tq; a.Tk = d->Tk; a.Hq = d->Hq; a.Hk = d->Hk; a.d = d->d; a.k_h = d->k_h; a.dtype = d->dtype;
     if ((rc = strides_of(d->q_stride, d->Hq, d->Tq, d->d, d->dtype, a.qs)) != SENTRY_OK) return rc;
     if ((rc = strides_of(d->k_stride, d->Hk, d->Tk, d->d, d->dtype, a.ks)) != SENTRY_OK) return rc;
-    return strides_of(d->v_stride, d->Hk, d->Tk, d->d, d->dtype, a.vs);
+    if ((rc = strides_of(d->v_stride, d->Hk, d->Tk, d->d, d->dtype, a.vs)) != SENTRY_OK) return rc;
+    if (d->Tk > 1 && (a.ks[2] == 0 || a.vs[2] == 0)) return SENTRY_ERR_UNSUPPORTED;   // one key for all of them
+    return SENTRY_OK;
 }
 
 int check_cache(const sentry_kv_cache* c) {
@@ -49,6 +51,7 @@ int check_cache(const sentry_kv_cache* c) {
     if (!head_dim(c->d) || c->Hk > kServeMaxHeads) return SENTRY_ERR_UNSUPPORTED;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return SENTRY_ERR_UNSUPPORTED;
     if ((long long)c->max_pages * c->page > 0x7fffffffLL - 4096) return SENTRY_ERR_UNSUPPORTED;
+    if ((long long)c->n_pages * c->Hk > 0x7fffffffLL / c->page) return SENTRY_ERR_UNSUPPORTED;   // rows of the pool are counted in 32 bits
     return SENTRY_OK;
 }
 int check_cache_pointers(const sentry_kv_cache* c) {

@@ -1,22 +1,24 @@
 // Serving attention for few rows: a decoder's single tokens and short blocks, over dense 16-bit keys and values or the 8-bit cache.
 //
 // The rows of one KV group (kept heads x Tq) share its keys, so they are packed into tiles of 8 or 16 rows, and a block takes a tile and a
-// stretch of the keys.  Each of its four warps walks tiles of 32 keys by itself, with a ring of asynchronous copies of its own, a running
-// maximum and sum of its own (log2 domain), and both products on the warp MMA: no barrier until the four partial results meet.
-// Long axes are split over blocks; kv_combine_kernel joins the parts.
+// stretch of the keys.  One warp brings tiles of 32 keys into a ring by TMA, which also swizzles them against bank conflicts; four others
+// take them in turn, each with a running maximum and sum of its own (log2 domain) and both products on the warp MMA: no barrier between
+// them until the four partial results meet.  Long axes are shared out over blocks; kv_combine_kernel joins the parts.
 // The keys are the MMA's 16 rows and the queries its 8 columns (S^T = K Q^T, O^T = V^T P^T): a decoder's few rows fill it, where queries as
-// rows left half of it and half of the exponentials empty (two hours of cached tokens 31 us so, with 840 instructions a tile of 4 KB).
-// What bounds it: the bytes of K and V, read once from memory.  For that the codes go through registers straight into MMA operands:
-// the order of the inner index is free as long as both operands share it, so that a lane's 16 consecutive bytes of a key are its operand
-// for K's product; and for V's, where pairs run along the keys, two keys' words are interleaved byte by byte.  The weights get from the
-// first product's layout to the second's by a transposition of 8 x 8 matrices among registers.  8-bit codes become fp16 exactly; a
-// page's key scale multiplies the scores, its value scale the weights.  The maximum is followed only where a score exceeds it by 2^8.
+// rows left half of it and half of the exponentials empty.
+// What bounds it: the bytes of K and V, read once from memory, and the instructions that turn codes into operands.  They go from
+// shared memory through registers straight into the MMA: the order of the inner index is free as long as both operands share it, so that
+// a lane's 16 consecutive bytes of a key are its operand for K's product; and for V's, where pairs run along the keys, two keys'
+// words are interleaved byte by byte.  The weights get from the first product's layout to the second's by a transposition of 8 x 8
+// matrices among registers.  8-bit codes become fp16 exactly; a page's key scale multiplies the scores, its value scale the weights.
+// The maximum is followed only where a score exceeds it by 2^8.
+// Every wait is bounded; on expiry the block raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
-#include "ptx/sm100.cuh"
+#include "kv_maps.cuh"
 
 namespace {
 
-constexpr int kWarps = 4, kKeys = 32;
+constexpr int kWarps = 4, kKeys = 32, kRowsThreads = (kWarps + 1) * 32;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2, KV_I8 = 3 };
@@ -25,31 +27,20 @@ template <int KV, int D>
 struct RowsCfg {
     static constexpr int ESIZE = KV <= KV_F16 ? 2 : 1;
     static constexpr int ROW = D * ESIZE;                    // bytes of a key
-    static constexpr int CHUNKS = ROW / 16;
-    static constexpr int STAGE = 2 * kKeys * ROW;            // K and V of a tile
-    // Two tiles of copies on the way for every warp at least, and as many blocks on an SM as that leaves room for.
-    static constexpr int FIT = 49152 / (kWarps * STAGE);
-    static constexpr int STAGES = FIT < 2 ? (STAGE > 8192 ? 3 : 2) : FIT > 4 ? 4 : FIT;
-    static constexpr int BLOCKS = STAGE > 8192 ? 1 : FIT < 2 ? 3 : 4;
-    static constexpr int RING = kWarps * STAGES * STAGE;
+    static constexpr int RB = ROW < 128 ? ROW : 128;         // of a row in shared memory; wider keys lie in slabs
+    static constexpr int TILE = kKeys * ROW < 1024 ? 1024 : kKeys * ROW;   // of K or V, on the swizzle's boundary
+    // tiles of the ring (two for each warp at least, but for 16-bit rows of 128), and blocks on an SM
+    static constexpr int STAGES = TILE > 4096 ? 6 : TILE > 2048 ? 8 : 12;
+    static constexpr int BLOCKS = TILE > 4096 ? 2 : TILE > 2048 ? 3 : 4;
+    static constexpr int RING = STAGES * 2 * TILE;
     static constexpr int MERGE = kWarps * 16 * D * 4;
-    static constexpr int SMEM = RING > MERGE ? RING : MERGE;
+    static constexpr int SMEM = (RING > MERGE ? RING : MERGE) + 1024;
 };
 
-// Piece c of key r lies at piece c ^ bank_shift(r) of its row: lanes that read one piece number of eight keys, or several of one, meet
-// different banks.  (Linear over XOR in the bits of r, so that constant parts of r shift by constants.)
-template <int CHUNKS>
-__host__ __device__ __forceinline__ constexpr int bank_shift(int r) {
-    return ((((r >> 1) & 3) * 2) ^ ((r & 1) * 4)) & (CHUNKS - 1);
-}
-__device__ __forceinline__ void cp_async_16_full(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool yes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(yes ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+// 16-byte piece c of key r lies at piece c ^ piece_shift(r) of its row of RB bytes (the copies' swizzle).
+template <int RB>
+__device__ __forceinline__ int piece_shift(int r) {
+    return RB == 128 ? r & 7 : RB == 64 ? (r >> 1) & 3 : RB == 32 ? (r >> 2) & 1 : 0;
 }
 template <int BYTES>
 __device__ __forceinline__ void lds(uint32_t addr, uint32_t* r) {
@@ -119,17 +110,16 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
 
 // Which stretch of which sample's keys a block takes.  The samples' lengths differ and only the device knows them, so that every block works
-// out the same shares: stretches of `chunk` tiles, as many blocks to a sample as it has of them (one at least), so that all fit one wave.
+// out the same shares: as many blocks to a sample as it has stretches of `chunk` tiles (one at least), so that all fit one wave.
 struct RowsShare { int b, split, n, first; };   // first: number of the sample's first part among all samples' parts
-__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room, int& chunk) {
+__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room) {
     const int lane = threadIdx.x & 31;
     auto tiles_of = [&](int b) { return b < a.B ? (kv_length(a, b) + kKeys - 1) / kKeys : 0; };
     int sum = 0;
 #pragma unroll 4
     for (int b0 = 0; b0 < a.B; b0 += 32) sum += tiles_of(b0 + lane);
     const long long total = (long long)__reduce_add_sync(0xffffffffu, sum >> 8) * 256 + __reduce_add_sync(0xffffffffu, sum & 255);
-    chunk = (int)((total + room - 1) / room);
-    chunk = max((chunk + kWarps - 1) / kWarps * kWarps, kWarps);
+    const int chunk = max((int)((total + room - 1) / room), kWarps);
     RowsShare r = {-1, 0, 0, 0};
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -158,25 +148,37 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
 // room: 0: a block per group and row tile takes all of its keys.  Otherwise the keys are shared out (rows_share), part: [parts][k_h][Tq][D] sums,
 // ml: [parts][k_h][Tq] (maximum, total), and plan: [B] (first part, parts) for those who join them.
 template <int KV, int D, bool BF16, int NT>
-__global__ void __launch_bounds__(kWarps * 32, NT == 1 ? RowsCfg<KV, D>::BLOCKS : RowsCfg<KV, D>::BLOCKS < 3 ? 1 : 3)
-kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, int room) {
+__global__ void __launch_bounds__(kRowsThreads, RowsCfg<KV, D>::BLOCKS - (NT > 1 && RowsCfg<KV, D>::BLOCKS > 2))
+kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, int room) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
     constexpr bool SPLIT_P = DENSE || !BF16;                 // weights as a head and a remainder
-    constexpr int KSTEPS = D / 16, DT = D / 16, ROWS = 8 * NT;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ RowsMeta s_meta[kWarps][C::STAGES];
+    constexpr int KSTEPS = D / 16, DT = D / 16, ROWS = 8 * NT, RB = C::RB;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ RowsMeta s_meta[C::STAGES];
+    __shared__ uint64_t s_kfull[C::STAGES], s_vfull[C::STAGES], s_kempty[C::STAGES], s_vempty[C::STAGES];
     __shared__ short s_head[kServeMaxHeads], s_pos[kServeMaxHeads];
-    __shared__ int s_heads;
+    __shared__ int s_heads, s_abort;
     __shared__ float s_m[kWarps][ROWS], s_l[kWarps][ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gq = lane >> 2, t4 = lane & 3;
     const int g = blockIdx.x % a.Hk;
+    const uint32_t raw_addr = ptx::smem_u32(smem_raw), ring = (raw_addr + 1023u) & ~1023u;
+    volatile int* abort_flag = &s_abort;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&s_kfull[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&s_vfull[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&s_kempty[s]), 1);
+            ptx::mbar_init(ptx::smem_u32(&s_vempty[s]), 1);
+        }
+        s_abort = 0;
+        ptx::fence_barrier_init();
+    }
     grid_dependents_start_if_small();
     grid_dependency_wait();
     RowsShare share = {(int)blockIdx.x / a.Hk, 0, 1, 0};
-    int chunk = 0x7fffffff / kKeys;
-    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room, chunk);   // (every warp for itself)
+    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room);       // (every warp for itself)
     if (share.b < 0) return;
     const int b = share.b;
     if (warp == 0) {
@@ -185,123 +187,93 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
         if (room > 0 && lane == 0 && share.split == 0 && g == 0 && blockIdx.y == 0) plan[b] = make_int2(share.first, share.n);
     }
     const int len = kv_length(a, b);
-    const uint32_t mask = a.masks ? a.masks[b] : 0u;
+    const int tiles = (len + kKeys - 1) / kKeys;
+    const int t0 = (int)((long long)tiles * share.split / share.n), t1 = (int)((long long)tiles * (share.split + 1) / share.n);
     __syncthreads();
     const int rows = s_heads * a.Tq;
-    const int tiles = (len + kKeys - 1) / kKeys;
-    const int t0 = min(share.split * chunk, tiles), t1 = min(t0 + chunk, tiles);
-    const uint32_t ring = ptx::smem_u32(smem) + warp * C::STAGES * C::STAGE;
-    RowsMeta* meta = s_meta[warp];
-    const char *kbase, *vbase;
-    if constexpr (DENSE) {
-        kbase = (const char*)a.K + (b * a.ks[0] + g * a.ks[1]) * 2;
-        vbase = (const char*)a.V + (b * a.vs[0] + g * a.vs[1]) * 2;
-    } else {
-        kbase = (const char*)a.K;
-        vbase = (const char*)a.V;
-    }
-    const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
-    const int32_t* pages = DENSE ? nullptr : a.table + (size_t)b * a.max_pages;
+    uint32_t done = 0;                                      // tiles of the row tiles before
 
-    for (int row0 = blockIdx.y * ROWS; row0 < rows; row0 += gridDim.y * ROWS) {
-        // -------------------------------------------------------------------- copies
-        // `ahead`: the modality id, or the page, of this lane's key of the tile that is issued next
-        auto look_ahead = [&](int tile) -> int {
-            const int n = tile * kKeys + lane;
-            if (tile >= t1 || n >= len) return -1;
-            if constexpr (DENSE) return a.ids ? a.ids[n] : 0;
-            else return pages[n >> page_shift];
-        };
-        // where this lane's first piece of a tile goes, and the distance between its pieces (32 lanes x 16 bytes: 32 / CHUNKS keys)
-        constexpr int RPI = 32 / C::CHUNKS;
-        const int my_row = lane / C::CHUNKS, my_chunk = lane % C::CHUNKS;
-        const int my_dst = my_row * C::ROW + ((my_chunk ^ bank_shift<C::CHUNKS>(my_row)) << 4);
-        // K's and V's copies of a tile are two groups: the slot of K is free, and filled again, half a tile before that of V
-        int next = t0 + warp, next_slot = 0, ahead = look_ahead(next);
-        unsigned next_vis = 0;
-        // this lane's first piece of the tile: of a dense tensor, or of a page and group (the pieces of a page's tile follow one another)
-        const char *k_first = kbase, *v_first = vbase;
-        long long k_step = 0, v_step = 0;
-        unsigned id[2] = {0, 0}, in_page = 0;                         // pages of the tile's first 16 keys and of the others; bytes into the first
-        if constexpr (DENSE) {
-            k_step = a.ks[2] * 2; v_step = a.vs[2] * 2;
-            k_first += my_row * k_step + my_chunk * 16;
-            v_first += my_row * v_step + my_chunk * 16;
-        } else {
-            k_first += (long long)(g << page_shift) * D + (C::CHUNKS > 1 ? lane : lane & 15) * 16;
-            v_first += (long long)(g << page_shift) * D + (C::CHUNKS > 1 ? lane : lane & 15) * 16;
-        }
-        const unsigned page_bytes = DENSE ? 0u : (unsigned)(a.Hk << page_shift) * D;    // of all groups: below 2^32
-        auto issue = [&](bool is_v) {
-            if (next < t1) {
-                const uint32_t dst = ring + next_slot * C::STAGE + (is_v ? kKeys * C::ROW : 0);
-                const int n0 = next * kKeys;
-                if (!is_v) {
-                    RowsMeta* mt = meta + next_slot;
-                    bool ok = n0 + lane < len;
-                    if constexpr (DENSE) ok = ok && (a.ids == nullptr || kv_present(ahead, mask));
-                    else {
-                        const bool good = (unsigned)ahead < (unsigned)a.n_pages;
-                        if (ok && !good) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
-                        ok = ok && good;
+    for (int row0 = blockIdx.y * ROWS; row0 < rows; row0 += gridDim.y * ROWS, done += (uint32_t)(t1 - t0)) {
+        bool ok = true;
+        if (warp == kWarps) {
+            // ---------------------------------------------------------------- copies
+            const uint32_t mask = a.masks ? a.masks[b] : 0u;
+            const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
+            const int32_t* pages = DENSE ? nullptr : a.table + (size_t)b * a.max_pages;
+            const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
+            // of 32 tiles at a time, a lane each: the pages of the first 16 keys and of the others (-1: none), and their scales
+            int id0 = -1, id1 = -1;
+            float ks0 = 0.0f, ks1 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;
+            int ahead = DENSE && a.ids != nullptr && t0 * kKeys + lane < len ? a.ids[t0 * kKeys + lane] : 0;
+            uint32_t s = done % C::STAGES, use = done / C::STAGES;
+            for (int tile = t0; tile < t1 && ok; ++tile) {
+                const int n0 = tile * kKeys;
+                unsigned vis;
+                int at0 = 0, at1 = 0;
+                if constexpr (DENSE) {
+                    bool here = n0 + lane < len;
+                    if (a.ids != nullptr) {
+                        here = here && kv_present(ahead, mask);
+                        ahead = n0 + kKeys + lane < len ? a.ids[n0 + kKeys + lane] : 0;
                     }
-                    next_vis = __ballot_sync(0xffffffffu, ok);
-                    if (lane == 0) mt->vis = next_vis;
-                    if constexpr (!DENSE) {
-                        if ((lane & 15) == 0 && ok) {
-                            const size_t ph = (size_t)(unsigned)ahead * (unsigned)a.Hk + g;
-                            cp_async_4(ptx::smem_u32(&mt->ks[lane >> 4]), a.k_scales + ph);
-                            cp_async_4(ptx::smem_u32(&mt->vs[lane >> 4]), a.v_scales + ph);
-                        }
-                        id[0] = __shfl_sync(0xffffffffu, ahead, 0);
-                        id[1] = __shfl_sync(0xffffffffu, ahead, 16);
-                        in_page = (unsigned)(n0 & (a.page - 1)) * D;
+                    vis = __ballot_sync(0xffffffffu, here);
+                } else {
+                    const int turn = (tile - t0) & 31;
+                    if (turn == 0) {
+                        const int n = (tile + lane) * kKeys;
+                        id0 = tile + lane < t1 ? pages[n >> page_shift] : -1;
+                        id1 = page_shift > 4 ? id0 : tile + lane < t1 && n + 16 < len ? pages[(n >> 4) + 1] : -1;
+                        const bool bad0 = tile + lane < t1 && (unsigned)id0 >= (unsigned)a.n_pages, bad1 = tile + lane < t1 && n + 16 < len && (unsigned)id1 >= (unsigned)a.n_pages;
+                        if (bad0 || bad1) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                        if ((unsigned)id0 >= (unsigned)a.n_pages) id0 = -1;
+                        if ((unsigned)id1 >= (unsigned)a.n_pages) id1 = -1;
+                        if (id0 >= 0) { ks0 = a.k_scales[(size_t)id0 * a.Hk + g]; vs0 = a.v_scales[(size_t)id0 * a.Hk + g]; }
+                        if (id1 >= 0) { ks1 = a.k_scales[(size_t)id1 * a.Hk + g]; vs1 = a.v_scales[(size_t)id1 * a.Hk + g]; }
                     }
+                    at0 = __shfl_sync(0xffffffffu, id0, turn);
+                    at1 = __shfl_sync(0xffffffffu, id1, turn);
+                    vis = len - n0 >= 32 ? 0xffffffffu : (1u << (len - n0)) - 1u;
+                    if (at0 < 0) vis &= 0xffff0000u;
+                    if (at1 < 0) vis &= 0x0000ffffu;
                 }
-                if (next_vis != 0) {
-                    const char* base = is_v ? vbase : kbase;
-                    const char* first = is_v ? v_first : k_first;
-                    const long long step = is_v ? v_step : k_step;
-                    const char *lo = first, *hi = first;
-                    if constexpr (DENSE) lo += n0 * step;
-                    else {
-                        lo += (unsigned long long)id[0] * page_bytes + in_page;
-                        hi = a.page == 16 ? first + (unsigned long long)id[1] * page_bytes : lo + 16 * D;
+                ok = warp_wait(&s_kempty[s], (use & 1) ^ 1, abort_flag);
+                if (ok) {
+                    // (whoever reads the slot's scales and bits does so before it gives K's half back)
+                    if (!DENSE && lane == ((tile - t0) & 31)) {
+                        s_meta[s].ks[0] = ks0; s_meta[s].ks[1] = ks1;
+                        s_meta[s].vs[0] = vs0; s_meta[s].vs[1] = vs1;
                     }
-                    auto piece = [&](int i, const char*& src) {
-                        if constexpr (DENSE) src = lo + i * RPI * step;
-                        else if constexpr (C::CHUNKS == 1) src = lane < 16 ? lo : hi;
-                        else src = i < C::CHUNKS / 2 ? lo + i * 512 : hi + (i - C::CHUNKS / 2) * 512;
-                        return dst + (my_dst ^ (bank_shift<C::CHUNKS>(i * RPI) << 4)) + i * 512;
-                    };
-                    const char* src;
-                    if (next_vis == 0xffffffffu) {
+                    if (lane == 0) s_meta[s].vis = vis;
+                    __syncwarp();
+                    if (elect_one()) {
 #pragma unroll
-                        for (int i = 0; i < C::CHUNKS; ++i) {
-                            const uint32_t at = piece(i, src);
-                            cp_async_16_full(at, src);
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int i = 0; i < C::CHUNKS; ++i) {
-                            const uint32_t at = piece(i, src);
-                            const bool yes = (next_vis >> (i * RPI + my_row)) & 1u;
-                            cp_async_16_or_zero(at, yes ? src : base, yes);
+                        for (int is_v = 0; is_v < 2; ++is_v) {
+                            const CUtensorMap* map = is_v ? &maps.v : &maps.k;
+                            const uint32_t bar = ptx::smem_u32(is_v ? &s_vfull[s] : &s_kfull[s]), dst = ring + s * 2 * C::TILE + is_v * C::TILE;
+                            if (is_v && !ptx::mbar_wait(ptx::smem_u32(&s_vempty[s]), (use & 1) ^ 1, abort_flag)) break;
+                            if (vis == 0) { ptx::mbar_arrive(bar); continue; }
+                            if constexpr (DENSE) {
+                                ptx::mbar_arrive_expect_tx(bar, kKeys * C::ROW);
+#pragma unroll
+                                for (int c = 0; c < C::ROW / RB; ++c) tma_load_4d(dst + c * kKeys * RB, map, c * 64, n0, is_v ? vg : kg, is_v ? vb : kb, bar);
+                            } else if (page_shift > 4) {
+                                ptx::mbar_arrive_expect_tx(bar, kKeys * C::ROW);
+                                ptx::tma_load_2d(dst, map, 0, (at0 * a.Hk + g) * a.page + (n0 & (a.page - 1)), bar);
+                            } else {
+                                ptx::mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 16 * C::ROW);
+                                if (at0 >= 0) ptx::tma_load_2d(dst, map, 0, (at0 * a.Hk + g) * 16, bar);
+                                if (at1 >= 0) ptx::tma_load_2d(dst + 16 * C::ROW, map, 0, (at1 * a.Hk + g) * 16, bar);
+                            }
                         }
                     }
+                    __syncwarp();
+                    ok = __all_sync(0xffffffffu, *abort_flag == 0);
                 }
-                if (is_v) {
-                    next += kWarps;
-                    next_slot = next_slot + 1 == C::STAGES ? 0 : next_slot + 1;
-                    ahead = look_ahead(next);
-                }
+                if (++s == C::STAGES) { s = 0; ++use; }
             }
-            ptx::cp_async_commit();
-        };
-#pragma unroll 1
-        for (int s = 0; s < C::STAGES; ++s) { issue(false); issue(true); }
-
-        // -------------------------------------------------------------------- rows of Q as MMA operands: lane (gq, t4) has row gq of every eight
+        }
+        float o[DT][NT][4], m[NT][2], l[NT][2], vref = 0.0f;        // O is in units of vref (8-bit values; see below)
+        if (warp < kWarps) {
         uint32_t qf[NT][KSTEPS][2];
         float scale[NT][2];                                     // of rows 2 t4 and 2 t4 + 1, whose scores this lane will hold
         int last[NT][2];                                        // keys that they see end here
@@ -351,7 +323,6 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                 last[nt][x] = !DENSE && a.causal ? min(len, len - a.Tq + i + 1) : len;
             }
         }
-        float o[DT][NT][4], m[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             m[nt][0] = m[nt][1] = -INFINITY;
@@ -365,10 +336,13 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
         constexpr int VB = D / 8 * C::ESIZE;                        // bytes of a key of V that a lane takes
         constexpr int PIECE = VB < 16 ? VB : 16, PIECES = VB / PIECE, WORDS = VB < 4 ? 1 : VB / 4;
         constexpr int KB = C::ROW / 4 < 16 ? C::ROW / 4 : 16;       // of a key of K, at a time
-        const int k_at = gq * C::ROW + ((((t4 * KB) >> 4) ^ bank_shift<C::CHUNKS>(gq)) << 4) + ((t4 * KB) & 15);
+        const int k_at = gq * RB + ((((t4 * KB) >> 4) ^ piece_shift<RB>(gq)) << 4) + ((t4 * KB) & 15);
         int v_at[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) v_at[u] = (2 * t4 + u) * C::ROW + ((((gq * VB) >> 4) ^ bank_shift<C::CHUNKS>(2 * t4 + u)) << 4) + ((gq * VB) & 15);
+        for (int u = 0; u < 2; ++u) {
+            const int at = gq * VB;
+            v_at[u] = at / RB * (kKeys * RB) + (2 * t4 + u) * RB + (((at % RB >> 4) ^ piece_shift<RB>(2 * t4 + u)) << 4) + (at & 15);
+        }
         // keys below this are seen by every row of the warp
         int all_see = len;
         if (!DENSE && a.causal) {
@@ -376,20 +350,20 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
             for (int nt = 0; nt < NT; ++nt) all_see = min(all_see, min(last[nt][0], last[nt][1]));
             all_see = __reduce_min_sync(0xffffffffu, all_see);
         }
-        float vref = 0.0f, inv_vref = 0.0f;                         // O is in units of vref (8-bit values; see below)
+        float inv_vref = 0.0f;
 
         // -------------------------------------------------------------------- tiles of 32 keys
-        int slot = 0;
         for (int tile = t0 + warp; tile < t1; tile += kWarps) {
-            ptx::cp_async_wait_group<2 * C::STAGES - 1>();
-            __syncwarp();
+            const uint32_t n = done + (uint32_t)(tile - t0), slot = n % C::STAGES, parity = n / C::STAGES & 1;
+            if (!warp_wait(&s_kfull[slot], parity, abort_flag)) break;
             const int n0 = tile * kKeys;
-            const uint32_t kt = ring + slot * C::STAGE, vt = kt + kKeys * C::ROW;
-            const unsigned vis = meta[slot].vis;
-            const float vscale[2] = {DENSE ? 1.0f : meta[slot].vs[0], DENSE ? 1.0f : meta[slot].vs[1]};
-            const bool full = vis == 0xffffffffu && n0 + kKeys <= all_see;
+            const uint32_t kt = ring + slot * 2 * C::TILE, vt = kt + C::TILE;
+            const unsigned vis = s_meta[slot].vis;
+            const float kscale[2] = {DENSE ? 1.0f : s_meta[slot].ks[0], DENSE ? 1.0f : s_meta[slot].ks[1]};
+            const float vscale[2] = {DENSE ? 1.0f : s_meta[slot].vs[0], DENSE ? 1.0f : s_meta[slot].vs[1]};
+            const bool any = __any_sync(0xffffffffu, vis != 0), full = __all_sync(0xffffffffu, vis == 0xffffffffu && n0 + kKeys <= all_see);
             float s[2][NT][4];
-            if (vis != 0) {
+            if (any) {
                 // ------ scores: element (key mt * 16 + gq + 8 * (x >> 1), row nt * 8 + 2 t4 + (x & 1))
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
@@ -398,10 +372,11 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
 #pragma unroll
                         for (int x = 0; x < 4; ++x) s[mt][nt][x] = 0.0f;
 #pragma unroll
-                    for (int c = 0; c < (C::CHUNKS + 3) / 4; ++c) {
+                    for (int c = 0; c < (C::ROW + 63) / 64; ++c) {
                         uint32_t w0[4], w1[4];                      // keys gq and gq + 8
-                        lds<KB>(kt + (k_at ^ (c * 64)) + mt * 16 * C::ROW, w0);
-                        lds<KB>(kt + (k_at ^ (c * 64)) + (mt * 16 + 8) * C::ROW, w1);
+                        const uint32_t at = kt + c / (RB / 64 > 0 ? RB / 64 : 1) * (kKeys * RB) + (k_at ^ (c % (RB / 64 > 0 ? RB / 64 : 1) * 64)) + mt * 16 * RB;
+                        lds<KB>(at, w0);
+                        lds<KB>(at + 8 * RB, w1);
 #pragma unroll
                         for (int x = 0; x < KB / (DENSE ? 8 : 4); ++x) {
                             uint32_t f[4];
@@ -418,7 +393,7 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                 }
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
-                    const float ks = DENSE ? 1.0f : meta[slot].ks[mt];
+                    const float ks = kscale[mt];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         const float c0 = scale[nt][0] * ks, c1 = scale[nt][1] * ks;
@@ -427,9 +402,8 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                     }
                 }
             }
-            __syncwarp();
-            issue(false);
-            if (vis != 0) {
+            warp_arrive(&s_kempty[slot]);
+            if (any) {
                 if (!full) {
 #pragma unroll
                     for (int mt = 0; mt < 2; ++mt)
@@ -482,15 +456,14 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                             l[nt][x & 1] += s[mt][nt][x];
                         }
                 }
-                ptx::cp_async_wait_group<2 * C::STAGES - 1>();
-                __syncwarp();
+                if (!warp_wait(&s_vfull[slot], parity, abort_flag)) break;
                 // ------ values, 16 keys at a time: column gq * (D / 8) + 2 j is row gq of the MMA's tile j, the next column its row gq + 8
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
                     if constexpr (!DENSE) {
                         // The page's scale multiplies the weights, as a ratio to vref; where it is far from that, O changes its unit.
                         // (A page 2^64 times smaller leaves it: its values are nothing beside what O may hold.)
-                        if (((vis >> (kk * 16)) & 0xffffu) == 0) continue;
+                        if (!full && ((vis >> (kk * 16)) & 0xffffu) == 0) continue;
                         const float vs = vscale[kk];
                         float ratio = vs * inv_vref;
                         if (!(fabsf(ratio) >= 0.0625f && fabsf(ratio) <= 16.0f)) {
@@ -538,7 +511,16 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
 #pragma unroll
-                        for (int y = 0; y < PIECES; ++y) lds<PIECE>(vt + (v_at[x & 1] ^ (y * 16)) + (kk * 16 + (x >> 1) * 8) * C::ROW, &v[x][y * 4]);
+                        for (int y = 0; y < PIECES; ++y) lds<PIECE>(vt + (v_at[x & 1] ^ (y * 16)) + (kk * 16 + (x >> 1) * 8) * RB, &v[x][y * 4]);
+                    if (!full) {
+                        // what absent keys hold may not be a number, which a weight of zero does not make one
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (!((vis >> (kk * 16 + 2 * t4 + (x & 1) + (x >> 1) * 8)) & 1u)) {
+#pragma unroll
+                                for (int y = 0; y < WORDS; ++y) v[x][y] = 0u;
+                            }
+                    }
                     auto product = [&](int j, const uint32_t (&f)[4]) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
@@ -580,14 +562,14 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                     }
                 }
             }
-            __syncwarp();
-            issue(true);
-            slot = slot + 1 == C::STAGES ? 0 : slot + 1;
+            if (!any && !warp_wait(&s_vfull[slot], parity, abort_flag)) break;
+            warp_arrive(&s_vempty[slot]);
         }
-        ptx::cp_async_wait_all();
+        }
         // -------------------------------------------------------------------- the four warps' parts
-        __syncthreads();                       // every ring has been read
-        float* so = reinterpret_cast<float*>(smem);
+        __syncthreads();                       // every tile has been read
+        float* so = reinterpret_cast<float*>(smem_raw + (ring - raw_addr));
+        if (warp < kWarps) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -602,8 +584,9 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                     *reinterpret_cast<float2*>(so + (warp * ROWS + r) * D + gq * (D / 8) + 2 * j) = make_float2(o[j][nt][x] * f, o[j][nt][x + 2] * f);
                 }
             }
+        }
         __syncthreads();
-        for (int e = threadIdx.x; e < ROWS * D / 2; e += kWarps * 32) {
+        for (int e = threadIdx.x; e < ROWS * D / 2; e += kRowsThreads) {
             const int r = e / (D / 2), c = e % (D / 2) * 2, row = row0 + r;
             if (row >= rows) break;
             float top = -INFINITY;
@@ -629,7 +612,14 @@ kv_rows_kernel(const KvAttendArgs a, float* __restrict__ part, float2* __restric
                 if (c == 0) ml[at] = make_float2(top, sum);
             }
         }
+        ptx::fence_proxy_async_smem();          // the next rows' copies come where these parts lay
         __syncthreads();
+        if (*abort_flag) break;
+    }
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicOr(a.status, SENTRY_STATUS_BIT_TIMEOUT);
+        const long long start = clock64();      // copies that are still on their way land before the shared memory goes
+        while (clock64() - start < 2000000LL) __nanosleep(1000);
     }
 }
 
@@ -645,8 +635,9 @@ long long rows_tiles(const KvAttendArgs& a) {
 }
 // Blocks that one wave holds for every row tile (RowsCfg::BLOCKS an SM); 0: the groups alone fill it, and no axis is split.
 int rows_wave(const KvAttendArgs& a) {
-    const int stage = 2 * kKeys * a.d * (a.format == 0 ? 2 : 1);
-    const long long slots = (stage > 8192 ? 1 : stage > 6144 || rows_tile(a) > 8 ? 3 : 4) * kSmCount, wave = rows_tiles(a) > 0 ? slots / rows_tiles(a) : 0;
+    const int tile = kKeys * a.d * (a.format == 0 ? 2 : 1);
+    const int blocks = tile > 4096 ? 2 : (tile > 2048 ? 3 : 4) - (rows_tile(a) > 8);
+    const long long slots = blocks * kSmCount, wave = rows_tiles(a) > 0 ? slots / rows_tiles(a) : 0;
     return a.B < wave / a.Hk && a.Tk > kWarps * kKeys ? (int)wave : 0;
 }
 
@@ -664,12 +655,16 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
         plan = ws.take<int2>(a.B);
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
+    KvMaps maps = {};
+    if (KV <= KV_F16 ? a.Tk > 0 && (!make_map_dense(&maps.k, a.K, a, a.ks, kKeys) || !make_map_dense(&maps.v, a.V, a, a.vs, kKeys))
+                     : a.n_pages > 0 && (!make_map_codes(&maps.k, a.K, a, a.page < kKeys ? a.page : kKeys) || !make_map_codes(&maps.v, a.V, a, a.page < kKeys ? a.page : kKeys)))
+        return SENTRY_ERR_CUDA;
     auto k = kv_rows_kernel<KV, D, BF16, NT>;
     static std::atomic<unsigned long long> allowed{0};
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
-        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kWarps * 32), C::SMEM, st, a, part, ml,
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kRowsThreads), C::SMEM, st, maps, a, part, ml,
                                        plan, wave > 0 ? room : 0));
     }
     return wave > 0 ? launch_kv_combine(ctx, a, part, ml, plan, 0, st) : SENTRY_OK;

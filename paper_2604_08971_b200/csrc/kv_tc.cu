@@ -11,10 +11,8 @@
 // K and V come by TMA where 128 present keys follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
 // where they do not: the last tile of a sample, and tiles across the border of a missing modality.
 // Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
-#include <cuda.h>
-
 #include "kv_attend.cuh"
-#include "tc_common.cuh"
+#include "kv_maps.cuh"
 
 namespace {
 
@@ -49,17 +47,9 @@ __device__ __forceinline__ uint32_t tile_offset(int r, int c) {
     return (uint32_t)((c / PER) * (128 * RB) + r * RB + (((c % PER) ^ f) << 4));
 }
 
-struct TcMaps { CUtensorMap k, v; };
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, int x, int y, int z, int w, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-                 "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
-                 : "memory");
-}
-
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kTcThreads, 1)
-kv_tc_kernel(const __grid_constant__ TcMaps maps, const KvAttendArgs a, const int32_t* __restrict__ list, const int32_t* __restrict__ counts,
+kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const int32_t* __restrict__ list, const int32_t* __restrict__ counts,
              float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
     using C = TcCfg<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -381,20 +371,6 @@ __global__ void __launch_bounds__(1024) kv_plan_kernel(const KvAttendArgs a, int
     if (threadIdx.x == 0) counts[b] = base;
 }
 
-// K or V as (64 columns, 128 tokens) boxes of (d, token, head, batch); a dimension of stride 0 is one that every index shares.
-bool make_map_kv(CUtensorMap* tm, const void* ptr, const KvAttendArgs& a, const long long st[3], bool bf16) {
-    EncodeTiledFn fn = get_encode_fn();
-    if (fn == nullptr) return false;
-    const int rb = a.d >= 64 ? 128 : a.d * 2;
-    const CUtensorMapSwizzle sw = rb == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : rb == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
-    cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.Tk, st[1] ? (cuuint64_t)a.Hk : 1, st[0] ? (cuuint64_t)a.B : 1};
-    cuuint64_t strides[3] = {(cuuint64_t)st[2] * 2, (cuuint64_t)(st[1] ? st[1] : 8) * 2, (cuuint64_t)(st[0] ? st[0] : 8) * 2};
-    cuuint32_t box[4] = {(cuuint32_t)rb / 2, kTN, 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    return fn(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int group_rows(const KvAttendArgs& a) {
     const int per = a.Hq / a.Hk, heads = per < a.k_h ? per : a.k_h;
     const long long r = (long long)heads * a.Tq;
@@ -416,8 +392,8 @@ int tc_splits(const KvAttendArgs& a) {
 
 template <int D, bool BF16>
 int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
-    TcMaps maps;
-    if (!make_map_kv(&maps.k, a.K, a, a.ks, BF16) || !make_map_kv(&maps.v, a.V, a, a.vs, BF16)) return SENTRY_ERR_CUDA;
+    KvMaps maps;
+    if (!make_map_dense(&maps.k, a.K, a, a.ks, kTN) || !make_map_dense(&maps.v, a.V, a, a.vs, kTN)) return SENTRY_ERR_CUDA;
     const int n_splits = tc_splits(a);
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     float* part = nullptr;
@@ -460,7 +436,7 @@ int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
 }  // namespace
 
 bool kv_tc_takes(const KvAttendArgs& a) {
-    return a.format == 0 && a.dtype != SENTRY_F32 && a.Tk > 0 && a.ks[2] > 0 && a.vs[2] > 0 && group_rows(a) > 32;
+    return a.format == 0 && a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > 32;
 }
 size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     const int n = tc_splits(a);
