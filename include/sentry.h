@@ -69,7 +69,8 @@ typedef enum { SENTRY_F32 = 0, SENTRY_BF16 = 1, SENTRY_F16 = 2, SENTRY_FP8_E4M3 
                SENTRY_I8 = 4 /* cache codes only */ } sentry_dtype;
 
 /* Create / destroy a context bound to CUDA device `device`.  Creation
- * allocates one small device status word; nothing else. */
+ * allocates one small device block (the status word, and counters that are
+ * zero between calls); nothing else. */
 SENTRY_API int sentry_create(sentry_ctx** out, int device);
 SENTRY_API int sentry_destroy(sentry_ctx* ctx);
 

@@ -89,8 +89,11 @@ int sentry_create(sentry_ctx** out, int device) {
     cudaDeviceProp prop;
     if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) { delete c; return SENTRY_ERR_CUDA; }
     c->sm_count = prop.multiProcessorCount;
-    if (cudaMalloc((void**)&c->d_status, sizeof(unsigned int)) != cudaSuccess) { delete c; return SENTRY_ERR_CUDA; }
-    if (cudaMemset(c->d_status, 0, sizeof(unsigned int)) != cudaSuccess) {
+    // the status word, and counters behind it that are zero between calls
+    const size_t bytes = 256 + kCounters * sizeof(unsigned int);
+    if (cudaMalloc((void**)&c->d_status, bytes) != cudaSuccess) { delete c; return SENTRY_ERR_CUDA; }
+    c->d_counters = c->d_status + 64;
+    if (cudaMemset(c->d_status, 0, bytes) != cudaSuccess) {
         cudaFree(c->d_status);
         delete c;
         return SENTRY_ERR_CUDA;

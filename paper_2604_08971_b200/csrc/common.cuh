@@ -15,6 +15,8 @@
 // for itself asks the context's sm_count.
 constexpr int kSmCount = 148;
 
+constexpr int kCounters = 2048;
+
 // Kernel slots for launch accounting and optional per-kernel timing.
 enum KernelSlot {
     KS_GATE_ROWS = 0, KS_GATE_EXPAND, KS_ATT_SCORE, KS_ATT_SELECT, KS_ATT_CORE,
@@ -30,6 +32,7 @@ struct sentry_ctx {
     void* workspace;
     size_t workspace_bytes;
     unsigned int* d_status;  // device status word (SENTRY_STATUS_BIT_*)
+    unsigned int* d_counters;   // kCounters words that every kernel leaves at zero
     int last_launches;
     int sm_count;
     bool profiling;

@@ -29,6 +29,10 @@ __device__ __forceinline__ float code_value(uint8_t c) {
 // head get their zero rows here, and the status bit.
 __device__ __forceinline__ int kv_group_heads(const KvAttendArgs& a, int b, int g, bool first, short* head, short* pos) {
     const int lane = threadIdx.x & 31, per = a.Hq / a.Hk;
+    if (a.kept == nullptr) {
+        for (int i = lane; i < per; i += 32) head[i] = pos[i] = (short)(g * per + i);
+        return per;
+    }
     int n = 0;
     for (int j0 = 0; j0 < a.k_h; j0 += 32) {
         const int j = j0 + lane, h = j < a.k_h ? kv_head(a, b, j) : -2;

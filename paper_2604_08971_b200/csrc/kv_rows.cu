@@ -107,23 +107,39 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     return r;
 }
 
-struct RowsMeta { float ks[2], vs[2]; unsigned vis; };
-
 // Which stretch of which sample's keys a block takes.  The samples' lengths differ and only the device knows them, so that every block works
 // out the same shares: as many blocks to a sample as it has stretches of `chunk` tiles (one at least), so that all fit one wave.
-struct RowsShare { int b, split, n, first; };   // first: number of the sample's first part among all samples' parts
-__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room) {
+struct RowsShare { int b, split, n, first, len; };   // first: number of the sample's first part among all samples' parts; len: its keys
+constexpr int kFusedParts = 16;
+__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room, bool fused) {
     const int lane = threadIdx.x & 31;
-    auto tiles_of = [&](int b) { return b < a.B ? (kv_length(a, b) + kKeys - 1) / kKeys : 0; };
-    int sum = 0;
+    auto length_of = [&](int b) { return b < a.B ? kv_length(a, b) : 0; };
+    auto tiles = [](int len) { return (len + kKeys - 1) / kKeys; };
+    const int mine = length_of(lane);
+    int sum = tiles(mine), top = sum;
 #pragma unroll 4
-    for (int b0 = 0; b0 < a.B; b0 += 32) sum += tiles_of(b0 + lane);
+    for (int b0 = 32; b0 < a.B; b0 += 32) {
+        const int t = tiles(length_of(b0 + lane));
+        sum += t;
+        top = max(top, t);
+    }
     const long long total = (long long)__reduce_add_sync(0xffffffffu, sum >> 8) * 256 + __reduce_add_sync(0xffffffffu, sum & 255);
-    const int chunk = max((int)((total + room - 1) / room), kWarps);
-    RowsShare r = {-1, 0, 0, 0};
+    int chunk = max((int)((total + room - 1) / room), kWarps);
+    if (a.B <= 32) {
+        // the smallest stretch with which all fit; the one above leaves out that few samples are a whole number of stretches
+        int low = max((int)(total / (room + a.B)), kWarps);
+        for (int step = 0; step < 6 && low < chunk; ++step) {
+            const int mid = (low + chunk) / 2;
+            const int n = __reduce_add_sync(0xffffffffu, lane < a.B ? max(1, (tiles(mine) + mid - 1) / mid) : 0);
+            if (n <= room + a.B) chunk = mid;
+            else low = mid + 1;
+        }
+    }
+    if (fused) chunk = max(chunk, (__reduce_max_sync(0xffffffffu, top) + kFusedParts - 1) / kFusedParts);
+    RowsShare r = {-1, 0, 0, 0, 0};
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int b = b0 + lane, n = b < a.B ? max(1, (tiles_of(b) + chunk - 1) / chunk) : 0;
+        const int b = b0 + lane, len = b0 ? length_of(b) : mine, n = b < a.B ? max(1, (tiles(len) + chunk - 1) / chunk) : 0;
         int incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -136,6 +152,7 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
             r.b = b0 + who;
             r.first = base + __shfl_sync(0xffffffffu, incl - n, who);
             r.n = __shfl_sync(0xffffffffu, n, who);
+            r.len = __shfl_sync(0xffffffffu, len, who);
             r.split = unit - r.first;
             break;
         }
@@ -144,19 +161,20 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
     return r;
 }
 
-// KV: type of the keys and values; BF16: type of Q and O; NT: tiles of 8 rows a block takes at a time.
 // room: 0: a block per group and row tile takes all of its keys.  Otherwise the keys are shared out (rows_share), part: [parts][k_h][Tq][D] sums,
-// ml: [parts][k_h][Tq] (maximum, total), and plan: [B] (first part, parts) for those who join them.
+// ml: [parts][k_h][Tq] (maximum, total).  The parts of a group's rows are joined by the last of its blocks (counters: one for each group and row
+// tile, left at zero), or, where a sample may have many, by kv_combine_kernel, for which plan: [B] says (first part, parts).
 template <int KV, int D, bool BF16, int NT>
 __global__ void __launch_bounds__(kRowsThreads, RowsCfg<KV, D>::BLOCKS - (NT > 1 && RowsCfg<KV, D>::BLOCKS > 2))
-kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, int room) {
+kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, unsigned int* __restrict__ counters,
+               int room) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
     constexpr bool SPLIT_P = DENSE || !BF16;                 // weights as a head and a remainder
     constexpr int KSTEPS = D / 16, DT = D / 16, ROWS = 8 * NT, RB = C::RB;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ RowsMeta s_meta[C::STAGES];
+    __shared__ unsigned s_vis[C::STAGES];                   // keys of the slot's tile that are there
     __shared__ uint64_t s_kfull[C::STAGES], s_vfull[C::STAGES], s_kempty[C::STAGES], s_vempty[C::STAGES];
     __shared__ short s_head[kServeMaxHeads], s_pos[kServeMaxHeads];
     __shared__ int s_heads, s_abort;
@@ -175,18 +193,21 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
         s_abort = 0;
         ptx::fence_barrier_init();
     }
-    grid_dependents_start_if_small();
+    // those who join the parts are few and small: their launch need not wait for this one's end
+    if (plan != nullptr && (long long)a.B * a.k_h * a.Tq <= 1024) grid_dependents_start();
+    else grid_dependents_start_if_small();
     grid_dependency_wait();
-    RowsShare share = {(int)blockIdx.x / a.Hk, 0, 1, 0};
-    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room);       // (every warp for itself)
+    RowsShare share = {(int)blockIdx.x / a.Hk, 0, 1, 0, 0};
+    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room, counters != nullptr);       // (every warp for itself)
+    else share.len = kv_length(a, share.b);
     if (share.b < 0) return;
     const int b = share.b;
     if (warp == 0) {
         const int n = kv_group_heads(a, b, g, g == 0 && share.split == 0 && blockIdx.y == 0, s_head, s_pos);
         if (lane == 0) s_heads = n;
-        if (room > 0 && lane == 0 && share.split == 0 && g == 0 && blockIdx.y == 0) plan[b] = make_int2(share.first, share.n);
+        if (plan != nullptr && lane == 0 && share.split == 0 && g == 0 && blockIdx.y == 0) plan[b] = make_int2(share.first, share.n);
     }
-    const int len = kv_length(a, b);
+    const int len = share.len;
     const int tiles = (len + kKeys - 1) / kKeys;
     const int t0 = (int)((long long)tiles * share.split / share.n), t1 = (int)((long long)tiles * (share.split + 1) / share.n);
     __syncthreads();
@@ -201,9 +222,8 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
             const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
             const int32_t* pages = DENSE ? nullptr : a.table + (size_t)b * a.max_pages;
             const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
-            // of 32 tiles at a time, a lane each: the pages of the first 16 keys and of the others (-1: none), and their scales
+            // of 32 tiles at a time, a lane each: the pages of the first 16 keys and of the others (-1: none)
             int id0 = -1, id1 = -1;
-            float ks0 = 0.0f, ks1 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;
             int ahead = DENSE && a.ids != nullptr && t0 * kKeys + lane < len ? a.ids[t0 * kKeys + lane] : 0;
             uint32_t s = done % C::STAGES, use = done / C::STAGES;
             for (int tile = t0; tile < t1 && ok; ++tile) {
@@ -227,8 +247,6 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
                         if (bad0 || bad1) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
                         if ((unsigned)id0 >= (unsigned)a.n_pages) id0 = -1;
                         if ((unsigned)id1 >= (unsigned)a.n_pages) id1 = -1;
-                        if (id0 >= 0) { ks0 = a.k_scales[(size_t)id0 * a.Hk + g]; vs0 = a.v_scales[(size_t)id0 * a.Hk + g]; }
-                        if (id1 >= 0) { ks1 = a.k_scales[(size_t)id1 * a.Hk + g]; vs1 = a.v_scales[(size_t)id1 * a.Hk + g]; }
                     }
                     at0 = __shfl_sync(0xffffffffu, id0, turn);
                     at1 = __shfl_sync(0xffffffffu, id1, turn);
@@ -238,12 +256,8 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
                 }
                 ok = warp_wait(&s_kempty[s], (use & 1) ^ 1, abort_flag);
                 if (ok) {
-                    // (whoever reads the slot's scales and bits does so before it gives K's half back)
-                    if (!DENSE && lane == ((tile - t0) & 31)) {
-                        s_meta[s].ks[0] = ks0; s_meta[s].ks[1] = ks1;
-                        s_meta[s].vs[0] = vs0; s_meta[s].vs[1] = vs1;
-                    }
-                    if (lane == 0) s_meta[s].vis = vis;
+                    // (whoever reads the slot's bits does so before it gives K's half back)
+                    if (lane == 0) s_vis[s] = vis;
                     __syncwarp();
                     if (elect_one()) {
 #pragma unroll
@@ -351,16 +365,34 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
             all_see = __reduce_min_sync(0xffffffffu, all_see);
         }
         float inv_vref = 0.0f;
+        // scales of this warp's next 32 tiles, a lane each (of the first 16 keys and of the others; 0 where there is no page)
+        float ks0 = 1.0f, ks1 = 1.0f, vs0 = 1.0f, vs1 = 1.0f;
+        int turn = 0;
 
         // -------------------------------------------------------------------- tiles of 32 keys
         for (int tile = t0 + warp; tile < t1; tile += kWarps) {
             const uint32_t n = done + (uint32_t)(tile - t0), slot = n % C::STAGES, parity = n / C::STAGES & 1;
+            if constexpr (!DENSE) {
+                if (turn == 0) {
+                    const int32_t* pages = a.table + (size_t)b * a.max_pages;
+                    const int mine = tile + lane * kWarps, n = mine * kKeys, shift = 31 - __clz(a.page);
+                    int id0 = mine < t1 ? pages[n >> shift] : -1, id1 = id0;
+                    if (shift == 4) id1 = mine < t1 && n + 16 < len ? pages[(n >> 4) + 1] : -1;
+                    ks0 = ks1 = vs0 = vs1 = 0.0f;
+                    if ((unsigned)id0 < (unsigned)a.n_pages) { ks0 = a.k_scales[(size_t)id0 * a.Hk + g]; vs0 = a.v_scales[(size_t)id0 * a.Hk + g]; }
+                    if ((unsigned)id1 < (unsigned)a.n_pages) { ks1 = a.k_scales[(size_t)id1 * a.Hk + g]; vs1 = a.v_scales[(size_t)id1 * a.Hk + g]; }
+                }
+            }
             if (!warp_wait(&s_kfull[slot], parity, abort_flag)) break;
             const int n0 = tile * kKeys;
             const uint32_t kt = ring + slot * 2 * C::TILE, vt = kt + C::TILE;
-            const unsigned vis = s_meta[slot].vis;
-            const float kscale[2] = {DENSE ? 1.0f : s_meta[slot].ks[0], DENSE ? 1.0f : s_meta[slot].ks[1]};
-            const float vscale[2] = {DENSE ? 1.0f : s_meta[slot].vs[0], DENSE ? 1.0f : s_meta[slot].vs[1]};
+            const unsigned vis = s_vis[slot];
+            float kscale[2] = {1.0f, 1.0f}, vscale[2] = {1.0f, 1.0f};
+            if constexpr (!DENSE) {
+                kscale[0] = __shfl_sync(0xffffffffu, ks0, turn); kscale[1] = __shfl_sync(0xffffffffu, ks1, turn);
+                vscale[0] = __shfl_sync(0xffffffffu, vs0, turn); vscale[1] = __shfl_sync(0xffffffffu, vs1, turn);
+                turn = (turn + 1) & 31;
+            }
             const bool any = __any_sync(0xffffffffu, vis != 0), full = __all_sync(0xffffffffu, vis == 0xffffffffu && n0 + kKeys <= all_see);
             float s[2][NT][4];
             if (any) {
@@ -616,6 +648,44 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
         __syncthreads();
         if (*abort_flag) break;
     }
+    if (counters != nullptr && share.n > 1) {
+        // the last block of the group and row tile to come here joins the parts
+        __threadfence();
+        __syncthreads();
+        unsigned int* counter = counters + ((size_t)b * a.Hk + g) * gridDim.y + blockIdx.y;
+        if (threadIdx.x == 0) s_heads = atomicAdd(counter, 1u) == (unsigned)share.n - 1u;
+        __syncthreads();
+        if (s_heads) {
+            __threadfence();
+            if (threadIdx.x == 0) *counter = 0u;
+            const size_t each = (size_t)a.k_h * a.Tq;
+            for (int row0 = blockIdx.y * ROWS; row0 < rows; row0 += gridDim.y * ROWS)
+                for (int e = threadIdx.x; e < min(ROWS, rows - row0) * (D / 4); e += kRowsThreads) {
+                    const int row = row0 + e / (D / 4), c = e % (D / 4) * 4;
+                    const size_t in = (size_t)s_pos[row / a.Tq] * a.Tq + row % a.Tq, first = (size_t)share.first * each + in;
+                    float top = -INFINITY, sum = 0.0f;
+                    float2 x[kFusedParts];
+#pragma unroll
+                    for (int s = 0; s < kFusedParts; ++s) {
+                        x[s] = s < share.n ? __ldcg(ml + first + s * each) : make_float2(-INFINITY, 0.0f);
+                        top = fmaxf(top, x[s].x);
+                    }
+                    const float ref = top == -INFINITY ? 0.0f : top;
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int s = 0; s < kFusedParts; ++s) {
+                        if (s >= share.n) break;
+                        const float f = exp2_fast(x[s].x - ref);
+                        const float4 p = __ldcg(reinterpret_cast<const float4*>(part + (first + s * each) * D + c));
+                        sum += x[s].y * f;
+                        v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+                    }
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    if (sum == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    *reinterpret_cast<uint2*>((uint16_t*)a.O + ((size_t)b * each + in) * D + c) = make_uint2(pack2<BF16>(v.x * inv, v.y * inv), pack2<BF16>(v.z * inv, v.w * inv));
+                }
+        }
+    }
     if (*abort_flag) {
         if (threadIdx.x == 0) atomicOr(a.status, SENTRY_STATUS_BIT_TIMEOUT);
         const long long start = clock64();      // copies that are still on their way land before the shared memory goes
@@ -641,10 +711,17 @@ int rows_wave(const KvAttendArgs& a) {
     return a.B < wave / a.Hk && a.Tk > kWarps * kKeys ? (int)wave : 0;
 }
 
+// Whether the last block of a group joins its parts: where the samples are enough that kFusedParts of each fill the wave.  (A launch of its own
+// costs 4 us behind the blocks' end; but one block is slow with a hundred parts.)
+bool rows_fused(const KvAttendArgs& a, int wave) {
+    return wave > 0 && (long long)a.B * kFusedParts >= wave / a.Hk && (long long)a.B * a.Hk * rows_tiles(a) <= kCounters;
+}
+
 template <int KV, int D, bool BF16, int NT>
 int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     using C = RowsCfg<KV, D>;
     const int wave = rows_wave(a), room = wave / a.Hk - a.B;      // parts beside the first of every sample
+    const bool fused = rows_fused(a, wave);
     const size_t rows = (size_t)a.k_h * a.Tq;
     float* part = nullptr;
     float2* ml = nullptr;
@@ -652,7 +729,7 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
     if (wave > 0) {
         part = ws.take<float>(wave / a.Hk * rows * D);
         ml = ws.take<float2>(wave / a.Hk * rows);
-        plan = ws.take<int2>(a.B);
+        if (!fused) plan = ws.take<int2>(a.B);
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
     KvMaps maps = {};
@@ -665,9 +742,9 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
         SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kRowsThreads), C::SMEM, st, maps, a, part, ml,
-                                       plan, wave > 0 ? room : 0));
+                                       plan, fused ? ctx->d_counters : nullptr, wave > 0 ? room : 0));
     }
-    return wave > 0 ? launch_kv_combine(ctx, a, part, ml, plan, 0, st) : SENTRY_OK;
+    return plan != nullptr ? launch_kv_combine(ctx, a, part, ml, plan, 0, st) : SENTRY_OK;
 }
 
 template <int KV, int D, bool BF16>
