@@ -1,14 +1,20 @@
 // Cross attention of many rows on the 5th-generation tensor cores (16-bit types).
 //
-// The rows of a KV group (kept heads x Tq) are packed; a CTA takes two tiles of 128 of them and walks the keys 128 at a time:
+// The rows of a KV group (kept heads x Tq) are packed; a CTA takes two tiles of 128 of them and walks the present keys, KN at a time:
 //   S_t = Q_t K^T        tcgen05, both operands in shared memory (128-byte rows, swizzled), S in tensor memory
-//   P_t = 2^(S c - m c)  a thread is a row: it reads its 128 scores, keeps its running maximum and sum, and writes the weights in 16 bits over
+//   P_t = 2^(S c - m c)  a thread is a row: it reads its scores, keeps its running maximum and sum, and writes the weights in 16 bits over
 //                        the scores that it has read
 //   O_t += P_t V         tcgen05, P from tensor memory, V as it lies in memory (MN-major)
 // Two tiles, so that the tensor core works for one while the other's rows are exponentiated.  The accumulator follows the running maximum
 // only where it grew by more than 2^8: until then weights are up to 2^8 instead of 1, which costs neither range nor precision, and
 // almost no iteration touches O.
-// K and V come by TMA where 128 present keys follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
+//
+// Bound by the exponentials (16 a clock and SM) up to d 64, by those and the products together at d 128.  Up to d 64 a step is of 64 keys and
+// an SM holds two CTAs, four tiles that wait for one another's latencies (4 x 4096 rows on 8192 keys, 16 heads on 4, d 64, bf16: 830 us, against
+// 910 with one CTA and 128 keys; 32 samples of 211 rows on 648 keys, 7 of 12 heads on 4: 28 us against 32); at d 128 tensor memory has room for
+// one, whose steps are of 128 keys (the same rows at d 128: 917 us in a burst, 1.2 PFLOP/s; 1050 under the power limit).  Registers hold all but the
+// last 32 scores of a step from the maximum to the weights: those are read twice (all of them at d 128: 945 us, with spills).
+// K and V come by TMA where the present keys of a step follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
 // where they do not: the last tile of a sample, and tiles across the border of a missing modality.
 // Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
@@ -16,19 +22,31 @@
 
 namespace {
 
-constexpr int kTM = 128, kTN = 128;          // rows of a tile, keys of a step
-constexpr int kTcThreads = 384;              // two softmax groups of four warps, three loading warps, one issuer
-constexpr int kLoadWarp0 = 8, kLoadWarps = 3, kIssueWarp = 11;
+constexpr int kTM = 128;                     // rows of a tile
 constexpr float kTcLog2e = 1.4426950408889634f;
+constexpr int kTcListed = 4096;              // keys whose list of present ones a CTA makes for itself
+
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {     // not a number if one of them is none
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 template <int D>
 struct TcCfg {
+    static constexpr int KN = D <= 64 ? 64 : 128;            // keys of a step
+    static constexpr int CTAS = KN == 64 ? 2 : 1;            // of an SM
+    static constexpr int LOAD_WARPS = KN == 64 ? 1 : 3;      // after the four softmax warps of each tile; then one issuer
+    static constexpr int LOAD_WARP0 = 8, ISSUE_WARP = LOAD_WARP0 + LOAD_WARPS, THREADS = (ISSUE_WARP + 1) * 32;
+    static constexpr int TMEM = 512 / CTAS, O_COL = 2 * KN;  // tensor memory: S of both tiles, then O of both
     static constexpr int RB = D >= 64 ? 128 : D * 2;         // bytes of a shared-memory row (64 elements at most)
     static constexpr int SLABS = D * 2 / RB;                 // column slabs of a tile
-    static constexpr int SLAB = 128 * RB;
-    static constexpr int TILE = SLABS * SLAB;                // 128 rows of D elements
+    static constexpr int SLAB = kTM * RB, TILE = SLABS * SLAB;         // of Q: 128 rows of D elements
+    static constexpr int KSLAB = KN * RB, KTILE = SLABS * KSLAB;       // of K and V
     static constexpr int STAGES = D == 128 ? 2 : 4;          // of K, and of V
-    static constexpr int SMEM = 2 * TILE + 2 * STAGES * TILE + 1024;
+    static constexpr int HELD = KN == 64 ? 1 : 3;            // blocks of 32 scores that a thread keeps from the maximum to the weights
+    static constexpr int SMEM = 2 * TILE + 2 * STAGES * KTILE + 1024;
+    static_assert(O_COL + 2 * D <= TMEM && (KN == 128 || SLABS == 1), "tensor memory, and slabs of 128 rows");
 };
 struct TcMisc {
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
@@ -37,6 +55,8 @@ struct TcMisc {
     int abort_flag;
     int n_heads;
     short head[kServeMaxHeads], pos[kServeMaxHeads];
+    int red[66];
+    uint16_t list[kTcListed];
 };
 
 // 16-byte piece c of row r in a tile of rows of RB bytes, swizzled in that row width's mode
@@ -48,23 +68,24 @@ __device__ __forceinline__ uint32_t tile_offset(int r, int c) {
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(TcCfg<D>::THREADS, TcCfg<D>::CTAS)
 kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const int32_t* __restrict__ list, const int32_t* __restrict__ counts,
              float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
     using C = TcCfg<D>;
+    constexpr int KN = C::KN;
     extern __shared__ uint8_t smem_raw[];
     __shared__ TcMisc misc_s;
     TcMisc* misc = &misc_s;
     volatile int* abort_flag = &misc->abort_flag;
     const uint32_t q_smem = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t k_smem = q_smem + 2 * C::TILE, v_smem = k_smem + C::STAGES * C::TILE;
+    const uint32_t k_smem = q_smem + 2 * C::TILE, v_smem = k_smem + C::STAGES * C::KTILE;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int split = blockIdx.x % n_splits, bg = blockIdx.x / n_splits, b = bg / a.Hk, g = bg % a.Hk;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
-            ptx::mbar_init(ptx::smem_u32(&misc->k_full[s]), kLoadWarps);
+            ptx::mbar_init(ptx::smem_u32(&misc->k_full[s]), C::LOAD_WARPS);
             ptx::mbar_init(ptx::smem_u32(&misc->k_empty[s]), 1);
-            ptx::mbar_init(ptx::smem_u32(&misc->v_full[s]), kLoadWarps);
+            ptx::mbar_init(ptx::smem_u32(&misc->v_full[s]), C::LOAD_WARPS);
             ptx::mbar_init(ptx::smem_u32(&misc->v_empty[s]), 1);
         }
         for (int t = 0; t < 2; ++t) {
@@ -85,8 +106,8 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
     __syncthreads();
     const int rows = misc->n_heads * a.Tq;
     if ((int)blockIdx.y * 2 * kTM >= rows) return;
-    if (warp == kIssueWarp) {
-        ptx::tmem_alloc(ptx::smem_u32(&misc->tmem_base), 512);
+    if (warp == C::ISSUE_WARP) {
+        ptx::tmem_alloc(ptx::smem_u32(&misc->tmem_base), C::TMEM);
         ptx::tmem_relinquish();
     }
     ptx::tc_fence_before_sync();
@@ -94,57 +115,73 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
     ptx::tc_fence_after_sync();
     const uint32_t tmem = misc->tmem_base;
 
-    // present keys of the sample, in order: those of the list, or the first `count`
-    const int32_t* at = list ? list + (size_t)b * a.Tk : nullptr;
-    const int count = list ? counts[b] : kv_length(a, b);
-    const int tiles = (count + kTN - 1) / kTN, per_split = (tiles + n_splits - 1) / n_splits;
+    // Q of a row block, by all threads
+    auto load_q = [&](int row0) {
+        const int halves = rows - row0 > kTM ? 2 : 1;
+        for (int e = threadIdx.x; e < halves * kTM * (D / 8); e += C::THREADS) {
+            const int r = e / (D / 8), c = e % (D / 8), row = row0 + r;
+            const uint32_t dst = q_smem + (r >> 7) * C::TILE + tile_offset<C::RB>(r & 127, c);
+            if (row < rows) {
+                const long long src = b * a.qs[0] + misc->head[row / a.Tq] * a.qs[1] + row % a.Tq * a.qs[2] + c * 8;
+                ptx::cp_async_16(dst, (const uint16_t*)a.Q + src);
+            } else {
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
+            }
+        }
+        ptx::cp_async_commit();
+    };
+    load_q(blockIdx.y * 2 * kTM);                 // (on its way while the list is made)
+    // present keys of the sample, in order: the first `count`, those of this CTA's list, or of one that was made before
+    const bool own = a.ids != nullptr && a.Tk <= kTcListed;
+    int count;
+    if (own) count = block_build_valid(a.ids, kv_length(a, b), a.masks[b], misc->list, misc->red);
+    else count = list ? counts[b] : kv_length(a, b);
+    const int32_t* far = list ? list + (size_t)b * a.Tk : nullptr;
+    auto key_at = [&](int p) { return own ? (int)misc->list[p] : far ? far[p] : p; };
+    const int tiles = (count + KN - 1) / KN, per_split = (tiles + n_splits - 1) / n_splits;
     const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles), steps = t1 - t0;
     uint32_t done = 0;                            // steps of the row blocks before
 
     for (int rb = blockIdx.y; rb * 2 * kTM < rows; rb += gridDim.y, done += (uint32_t)steps) {
         const int row0 = rb * 2 * kTM;
         const int halves = rows - row0 > kTM ? 2 : 1;
-        if (steps > 0) {
-            // ---------------------------------------------------------------- Q: all threads
-            for (int e = threadIdx.x; e < halves * kTM * (D / 8); e += kTcThreads) {
-                const int r = e / (D / 8), c = e % (D / 8), row = row0 + r;
-                const uint32_t dst = q_smem + (r >> 7) * C::TILE + tile_offset<C::RB>(r & 127, c);
-                if (row < rows) {
-                    const long long src = b * a.qs[0] + misc->head[row / a.Tq] * a.qs[1] + row % a.Tq * a.qs[2] + c * 8;
-                    ptx::cp_async_16(dst, (const uint16_t*)a.Q + src);
-                } else {
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
-                }
-            }
-            ptx::cp_async_wait_all();
-            ptx::fence_proxy_async_smem();
-            __syncthreads();
-        }
-        if (warp >= kLoadWarp0 && warp < kLoadWarp0 + kLoadWarps) {
+        if (rb != (int)blockIdx.y) load_q(row0);
+        ptx::cp_async_wait_all();
+        ptx::fence_proxy_async_smem();
+        __syncthreads();
+        if (warp >= C::LOAD_WARP0 && warp < C::LOAD_WARP0 + C::LOAD_WARPS) {
             // ---------------------------------------------------------------- K and V
-            const int lw = warp - kLoadWarp0;
+            const int lw = warp - C::LOAD_WARP0;
             const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
             bool ok = true;
+            // A tile that is gathered counts as here STAGES tiles (of K and V in turn) later, so that as many are on their way; what
+            // the tiles' users wait for meanwhile lies before those.
+            uint32_t gathered = 0;
+            auto arrive = [&](int i) {                      // (i: tiles of K and V in turn)
+                const uint32_t n = done + (i >> 1), s = n % C::STAGES;
+                ptx::fence_proxy_async_smem();
+                warp_arrive(i & 1 ? &misc->v_full[s] : &misc->k_full[s]);
+            };
             for (int j = 0; j < steps && ok; ++j) {
                 const uint32_t n = done + j, s = n % C::STAGES, use = n / C::STAGES;
-                const int p0 = (t0 + j) * kTN;
-                const bool full = p0 + kTN <= count;
-                const int first = at ? at[p0] : p0;
-                const bool together = full && (at == nullptr || at[p0 + kTN - 1] - first == kTN - 1);
+                const int p0 = (t0 + j) * KN;
+                const bool full = p0 + KN <= count;
+                const int first = key_at(p0);
+                const bool together = full && key_at(p0 + KN - 1) - first == KN - 1;
 #pragma unroll 1
                 for (int is_v = 0; is_v < 2 && ok; ++is_v) {
                     uint64_t* full_bar = is_v ? &misc->v_full[s] : &misc->k_full[s];
                     ok = warp_wait(is_v ? &misc->v_empty[s] : &misc->k_empty[s], (use & 1) ^ 1, abort_flag);
                     if (!ok) break;
-                    const uint32_t dst = (is_v ? v_smem : k_smem) + s * C::TILE;
+                    const uint32_t dst = (is_v ? v_smem : k_smem) + s * C::KTILE;
                     if (together) {
                         if (lw == 0) {
                             if (elect_one()) {
                                 const uint32_t bar = ptx::smem_u32(full_bar);
-                                ptx::mbar_arrive_expect_tx(bar, C::TILE);
+                                ptx::mbar_arrive_expect_tx(bar, C::KTILE);
 #pragma unroll
                                 for (int c = 0; c < C::SLABS; ++c)
-                                    tma_load_4d(dst + c * C::SLAB, is_v ? &maps.v : &maps.k, c * 64, first, is_v ? vg : kg, is_v ? vb : kb, bar);
+                                    tma_load_4d(dst + c * C::KSLAB, is_v ? &maps.v : &maps.k, c * 64, first, is_v ? vg : kg, is_v ? vb : kb, bar);
                             }
                             __syncwarp();
                         } else {
@@ -153,29 +190,36 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     } else {
                         const long long* st = is_v ? a.vs : a.ks;
                         const uint16_t* src = (const uint16_t*)(is_v ? a.V : a.K) + b * st[0] + g * st[1];
-                        for (int e = lw * 32 + lane; e < kTN * (D / 8); e += kLoadWarps * 32) {
+                        for (int e = lw * 32 + lane; e < KN * (D / 8); e += C::LOAD_WARPS * 32) {
                             const int r = e / (D / 8), c = e % (D / 8);
                             const uint32_t to = dst + tile_offset<C::RB>(r, c);
-                            if (p0 + r < count) ptx::cp_async_16(to, src + (at ? at[p0 + r] : p0 + r) * st[2] + c * 8);
+                            if (p0 + r < count) ptx::cp_async_16(to, src + key_at(p0 + r) * st[2] + c * 8);
                             else asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
                         }
-                        ptx::cp_async_wait_all();
-                        ptx::fence_proxy_async_smem();
-                        warp_arrive(full_bar);
+                    }
+                    ptx::cp_async_commit();
+                    gathered = gathered << 1 | !together;
+                    if (gathered >> C::STAGES & 1u) {
+                        ptx::cp_async_wait_group<C::STAGES>();
+                        arrive(2 * j + is_v - C::STAGES);
                     }
                 }
             }
-        } else if (warp == kIssueWarp) {
+            ptx::cp_async_wait_all();
+            if (ok)
+                for (int back = C::STAGES - 1; back >= 0; --back)
+                    if (gathered >> back & 1u) arrive(2 * steps - 1 - back);
+        } else if (warp == C::ISSUE_WARP) {
             // ---------------------------------------------------------------- UMMAs
-            constexpr uint32_t qk = BF16 ? ptx::umma_idesc_bf16(kTM, kTN) : ptx::umma_idesc_f16(kTM, kTN);
+            constexpr uint32_t qk = BF16 ? ptx::umma_idesc_bf16(kTM, KN) : ptx::umma_idesc_f16(kTM, KN);
             constexpr uint32_t pv = BF16 ? ptx::umma_idesc_bf16_major(kTM, D, false, true) : ptx::umma_idesc_f16_major(kTM, D, false, true);
             bool ok = true;
             auto scores = [&](int t, uint32_t s) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k * 32 / C::RB) * C::SLAB + k * 32 % C::RB;
-                    ptx::umma_bf16(tmem + t * kTN, ptx::umma_smem_desc_rows(q_smem + t * C::TILE + off, C::RB),
-                                   ptx::umma_smem_desc_rows(k_smem + s * C::TILE + off, C::RB), qk, k > 0 ? 1u : 0u);
+                    const uint32_t slab = k * 32 / C::RB, off = k * 32 % C::RB;
+                    ptx::umma_bf16(tmem + t * KN, ptx::umma_smem_desc_rows(q_smem + t * C::TILE + slab * C::SLAB + off, C::RB),
+                                   ptx::umma_smem_desc_rows(k_smem + s * C::KTILE + slab * C::KSLAB + off, C::RB), qk, k > 0 ? 1u : 0u);
                 }
                 ptx::umma_commit(ptx::smem_u32(&misc->s_full[t]));
             };
@@ -198,15 +242,14 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 ok = warp_wait(&misc->v_full[s], use & 1, abort_flag);
                 for (int t = 0; t < halves && ok; ++t) {
                     ok = warp_wait(&misc->p_full[t], n & 1, abort_flag);
-                    if (!ok) break;
-                    if (more && t == 0) ok = warp_wait(&misc->k_full[s2], use2 & 1, abort_flag);
+                    if (ok && more && t == 0) ok = warp_wait(&misc->k_full[s2], use2 & 1, abort_flag);
                     if (!ok) break;
                     ptx::tc_fence_after_sync();
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kTN / 16; ++k)
-                            ptx::umma_bf16_tmem_a(tmem + 256 + t * D, tmem + t * kTN + k * 8,
-                                                  ptx::umma_smem_desc_rows(v_smem + s * C::TILE + k * 16 * C::RB, C::RB, C::SLAB), pv, (j > 0 || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < KN / 16; ++k)
+                            ptx::umma_bf16_tmem_a(tmem + C::O_COL + t * D, tmem + t * KN + k * 8,
+                                                  ptx::umma_smem_desc_rows(v_smem + s * C::KTILE + k * 16 * C::RB, C::RB, C::KSLAB), pv, (j > 0 || k > 0) ? 1u : 0u);
                         ptx::umma_commit(ptx::smem_u32(&misc->o_full[t]));
                         if (t == halves - 1) ptx::umma_commit(ptx::smem_u32(&misc->v_empty[s]));
                         if (more) {
@@ -217,12 +260,12 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     __syncwarp();
                 }
             }
-        } else if (warp < 8) {
+        } else if (warp < C::LOAD_WARP0) {
             // ---------------------------------------------------------------- softmax: a thread is a row
             const int t = warp >> 2;
             const int row = row0 + t * kTM + (warp & 3) * 32 + lane;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            const uint32_t sc = tmem + t * kTN + lanes, oc = tmem + 256 + t * D + lanes;
+            const uint32_t sc = tmem + t * KN + lanes, oc = tmem + C::O_COL + t * D + lanes;
             const float c = rsqrtf((float)D) * kTcLog2e;
             // fp16 weights are taken 2^7 times as large (2^15 at most): its range is what small ones run out of
             constexpr float kShift = BF16 ? 0.0f : 7.0f;
@@ -233,26 +276,28 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 ok = warp_wait(&misc->s_full[t], n & 1, abort_flag);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                uint32_t s[kTN / 32][32];
+                const int valid = count - (t0 + j) * KN;
+                uint32_t s[KN / 32][32];
+                auto hide = [&](int z) {
+                    if (valid < KN) {
 #pragma unroll
-                for (int x = 0; x < kTN / 32; ++x) ptx::tmem_ld_32x32(sc + x * 32, s[x]);
+                        for (int y = 0; y < 32; ++y)
+                            if (z * 32 + y >= valid) s[z][y] = 0xff800000u;
+                    }
+                };
+#pragma unroll
+                for (int z = 0; z < KN / 32; ++z) ptx::tmem_ld_32x32(sc + z * 32, s[z]);
                 ptx::tmem_ld_wait();
-                const int valid = count - (t0 + j) * kTN;
-                if (valid < kTN) {
 #pragma unroll
-                    for (int x = 0; x < kTN; ++x)
-                        if (x >= valid) s[x / 32][x % 32] = 0xff800000u;
-                }
+                for (int z = 0; z < KN / 32; ++z) hide(z);
+                // (a score that is not a number makes the maximum one, and with it the whole row)
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int x = 0; x < kTN; x += 8)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        top[y] = fmaxf(top[y], fmaxf(__uint_as_float(s[x / 32][x % 32 + 2 * y]), __uint_as_float(s[x / 32][x % 32 + 2 * y + 1])));
-                const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+                for (int y = 0; y < KN; y += 2) top[(y >> 1) & 3] = max3_nan(top[(y >> 1) & 3], __uint_as_float(s[y / 32][y % 32]), __uint_as_float(s[y / 32][y % 32 + 1]));
+                const float now = max3_nan(max3_nan(m, top[0], top[1]), top[2], top[3]);
                 if (j == 0) m = now;
                 else {
-                    const bool grew = (now - m) * c > 8.0f;
+                    const bool grew = !((now - m) * c <= 8.0f);
                     if (__any_sync(0xffffffffu, grew)) {
                         // O follows the maximum; the last product into it has to be complete
                         ok = warp_wait(&misc->o_full[t], (n - 1) & 1, abort_flag);
@@ -262,73 +307,77 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                         m = now;
                         l *= keep;
 #pragma unroll
-                        for (int x = 0; x < D; x += 16) {
+                        for (int z = 0; z < D; z += 16) {
                             uint32_t o[16];
-                            ptx::tmem_ld_32x16(oc + x, o);
+                            ptx::tmem_ld_32x16(oc + z, o);
                             ptx::tmem_ld_wait();
 #pragma unroll
                             for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
-                            ptx::tmem_st_32x16(oc + x, o);
+                            ptx::tmem_st_32x16(oc + z, o);
                         }
                     }
                 }
                 const float mc = (m == -INFINITY ? 0.0f : m * c) - kShift;
-                float sum[4] = {};
+                const uint64_t cc = pair_f32(c, c), mcc = pair_f32(-mc, -mc), one = pair_f32(1.0f, 1.0f);
+                uint64_t sum[2] = {pair_f32(0.0f, 0.0f), pair_f32(0.0f, 0.0f)};
 #pragma unroll
-                for (int x = 0; x < kTN / 32; ++x) {
+                for (int z = 0; z < KN / 32; ++z) {
                     uint32_t w[16];
+                    if (z >= C::HELD) {                // (read again: the registers do not hold them all)
+                        ptx::tmem_ld_32x32(sc + z * 32, s[z]);
+                        ptx::tmem_ld_wait();
+                        hide(z);
+                    }
 #pragma unroll
                     for (int y = 0; y < 16; ++y) {
-                        const float p0 = exp2_fast(fmaf(__uint_as_float(s[x][2 * y]), c, -mc)), p1 = exp2_fast(fmaf(__uint_as_float(s[x][2 * y + 1]), c, -mc));
-                        sum[y & 1] += p0;
-                        sum[2 + (y & 1)] += p1;
+                        const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[z][2 * y]), __uint_as_float(s[z][2 * y + 1])), cc, mcc));
+                        const float p0 = exp2_fast(u.x), p1 = exp2_fast(u.y);
+                        sum[y & 1] = fma_pair(pair_f32(p0, p1), one, sum[y & 1]);
                         w[y] = pack2<BF16>(p0, p1);
                     }
-                    ptx::tmem_st_32x16(sc + x * 16, w);
+                    ptx::tmem_st_32x16(sc + z * 16, w);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const float2 sums[2] = {pair_of(sum[0]), pair_of(sum[1])};
+                l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 warp_arrive(&misc->p_full[t]);
             }
             // ---------------------------------------------------------------- results
-            if (t < halves) {
-                if (steps > 0 && ok) ok = warp_wait(&misc->o_full[t], (done + steps - 1) & 1, abort_flag);
-                ptx::tc_fence_after_sync();
-                if (ok) {
-                    const bool in = row < rows;
-                    const size_t each = (size_t)a.k_h * a.Tq, within = in ? (size_t)misc->pos[row / a.Tq] * a.Tq + row % a.Tq : 0;
-                    const size_t out = b * each + within, pat = ((size_t)b * n_splits + split) * each + within;
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * c - kShift, l) : make_float2(-INFINITY, 0.0f);
+            if (t < halves && steps > 0 && ok) ok = warp_wait(&misc->o_full[t], (done + steps - 1) & 1, abort_flag);
+            ptx::tc_fence_after_sync();
+            if (t < halves && ok) {
+                const bool in = row < rows;
+                const size_t each = (size_t)a.k_h * a.Tq, within = in ? (size_t)misc->pos[row / a.Tq] * a.Tq + row % a.Tq : 0;
+                const size_t out = b * each + within, pat = ((size_t)b * n_splits + split) * each + within;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * c - kShift, l) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-                    for (int x = 0; x < D; x += 16) {
-                        uint32_t o[16];
-                        if (steps > 0) {
-                            ptx::tmem_ld_32x16(oc + x, o);
-                            ptx::tmem_ld_wait();
-                        } else {
+                for (int z = 0; z < D; z += 16) {
+                    uint32_t o[16];
+                    if (steps > 0) {
+                        ptx::tmem_ld_32x16(oc + z, o);
+                        ptx::tmem_ld_wait();
+                    } else {
 #pragma unroll
-                            for (int y = 0; y < 16; ++y) o[y] = 0u;
-                        }
-                        if (!in) continue;
-                        if (n_splits == 1) {
-                            uint32_t w[8];
+                        for (int y = 0; y < 16; ++y) o[y] = 0u;
+                    }
+                    if (!in) continue;
+                    if (n_splits == 1) {
+                        uint32_t w[8];
 #pragma unroll
-                            for (int y = 0; y < 8; ++y)
-                                w[y] = l == 0.0f ? 0u : pack2<BF16>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
-                            uint4* dst = reinterpret_cast<uint4*>((uint16_t*)a.O + out * D + x);
-                            dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                            dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
-                        } else if (steps > 0) {
-                            uint4* dst = reinterpret_cast<uint4*>(part + pat * D + x);
+                        for (int y = 0; y < 8; ++y) w[y] = l == 0.0f ? 0u : pack2<BF16>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
+                        uint4* dst = reinterpret_cast<uint4*>((uint16_t*)a.O + out * D + z);
+                        dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                        dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    } else if (steps > 0) {
+                        uint4* dst = reinterpret_cast<uint4*>(part + pat * D + z);
 #pragma unroll
-                            for (int y = 0; y < 4; ++y) dst[y] = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
-                        }
+                        for (int y = 0; y < 4; ++y) dst[y] = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
                     }
                 }
-                ptx::tc_fence_before_sync();
             }
+            ptx::tc_fence_before_sync();
         }
         __syncthreads();                      // Q and O may be taken over
         ptx::tc_fence_after_sync();
@@ -341,9 +390,9 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
         while (clock64() - start < 2000000LL) __nanosleep(1000);
         __syncthreads();
     }
-    if (warp == kIssueWarp) {
+    if (warp == C::ISSUE_WARP) {
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc(tmem, 512);
+        ptx::tmem_dealloc(tmem, C::TMEM);
     }
 }
 
@@ -380,20 +429,24 @@ long long row_blocks(const KvAttendArgs& a) {
     const long long n = ((long long)group_rows(a) + 2 * kTM - 1) / (2 * kTM);
     return n > 65535 ? 65535 : n;
 }
+int tc_keys(int d) { return d <= 64 ? TcCfg<64>::KN : TcCfg<128>::KN; }
+int tc_ctas(int d) { return d <= 64 ? TcCfg<64>::CTAS : TcCfg<128>::CTAS; }
 // Blocks along the keys: where the row blocks alone leave SMs idle, each with two steps at least.
 int tc_splits(const KvAttendArgs& a) {
     const long long units = (long long)a.B * a.Hk * row_blocks(a);
-    const long long tiles = ((long long)a.Tk + kTN - 1) / kTN;
+    const long long tiles = ((long long)a.Tk + tc_keys(a.d) - 1) / tc_keys(a.d);
     if (units == 0) return 1;
-    long long n = kSmCount / units;
+    long long n = (long long)tc_ctas(a.d) * kSmCount / units;
     if (n > tiles / 2) n = tiles / 2;
     return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
+bool tc_planned(const KvAttendArgs& a) { return a.ids != nullptr && a.Tk > kTcListed; }
 
 template <int D, bool BF16>
 int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
+    using C = TcCfg<D>;
     KvMaps maps;
-    if (!make_map_dense(&maps.k, a.K, a, a.ks, kTN) || !make_map_dense(&maps.v, a.V, a, a.vs, kTN)) return SENTRY_ERR_CUDA;
+    if (!make_map_dense(&maps.k, a.K, a, a.ks, C::KN) || !make_map_dense(&maps.v, a.V, a, a.vs, C::KN)) return SENTRY_ERR_CUDA;
     const int n_splits = tc_splits(a);
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     float* part = nullptr;
@@ -403,22 +456,22 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
         part = ws.take<float>(n_splits * rows * D);
         ml = ws.take<float2>(n_splits * rows);
     }
-    if (a.ids != nullptr) {
+    if (tc_planned(a)) {
         list = ws.take<int32_t>((size_t)a.B * a.Tk);
         counts = ws.take<int32_t>(a.B);
     }
     if (!ws.ok) return SENTRY_ERR_WORKSPACE;
-    if (a.ids != nullptr) {
+    if (tc_planned(a)) {
         LaunchScope ls(ctx, KS_KV_PLAN, st);
         SENTRY_CUDA_TRY(launch_chained(kv_plan_kernel, dim3((unsigned)a.B), dim3(1024), 0, st, a, list, counts));
     }
     auto k = kv_tc_kernel<D, BF16>;
     static std::atomic<unsigned long long> allowed{0};
-    SENTRY_CUDA_TRY(allow_smem(k, TcCfg<D>::SMEM, ctx->device, allowed));
+    SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
-        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(kTcThreads), TcCfg<D>::SMEM, st, maps, a,
-                                       (const int32_t*)list, (const int32_t*)counts, part, ml, n_splits));
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(C::THREADS), C::SMEM, st, maps, a, (const int32_t*)list,
+                                       (const int32_t*)counts, part, ml, n_splits));
     }
     return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, nullptr, n_splits, st) : SENTRY_OK;
 }
@@ -443,6 +496,7 @@ size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     size_t bytes = 0;
     if (n > 1) bytes += align_up(n * rows * a.d * sizeof(float), 256) + align_up(n * rows * sizeof(float2), 256);
+    if (a.Tk <= kTcListed) return bytes + 512;
     // (whether the call has modality ids is not in the descriptor)
     return bytes + align_up((size_t)a.B * a.Tk * sizeof(int32_t), 256) + align_up((size_t)a.B * sizeof(int32_t), 256) + 512;
 }
