@@ -514,10 +514,12 @@ SENTRY_API int sentry_linear_i8(sentry_ctx* ctx, const sentry_linear_desc* desc,
  *   kept_heads [B,k_h] i32 or NULL (k_h == Hq, every head).  An entry outside [0,Hq) gives zero rows and BAD_INDEX.
  *   key_modality_ids [Tk] i32 + masks [B] u32, or both NULL; an id outside [0,32) is absent
  * Strides in elements, multiples of 8 for the 16-bit types and of 4 for F32 (a token's d values are contiguous; Q, K and V
- * may be views of one projection's result); all three 0 = contiguous.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
+ * may be views of one projection's result), at most 2^38; all three 0 = contiguous.  A batch or head stride of 0 shares one
+ * tensor; a token stride of 0 of K or V with Tk > 1 is UNSUPPORTED.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
  * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24.
- * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (relative 2^-9, 2^-12),
- * in the form for few rows as a rounded head and a remainder.
+ * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (by 2^-8 and 2^-11 of
+ * themselves at most), in the form for few rows as a rounded head and a remainder.  A row whose scores are all minus infinity
+ * (from an infinite q or k) is zero.
  * Workspace: sentry_cross_workspace_bytes.
  */
 typedef struct sentry_cross_desc {
@@ -543,7 +545,8 @@ SENTRY_API int sentry_cross_attend_fwd(sentry_ctx* ctx, const sentry_cross_desc*
  *                       page page_table[b, t / page].  Entries behind a sample's tokens are not read.  An entry outside
  *                       [0,n_pages) that is needed raises BAD_INDEX: nothing is stored there, its tokens are not seen.
  * Pages may be shared by samples that only read them (several decoders over one encoder's states).  A page that is
- * appended to belongs to one place of one sample alone.
+ * appended to belongs to one place of one sample alone.  n_pages * Hk * page and max_pages * page: below 2^31 (less 4096 for
+ * the latter), else UNSUPPORTED.
  */
 typedef struct sentry_kv_cache {
     int Hk, d, page, n_pages, max_pages; /* d in {16,32,64,128}, page in {16,32,64,128} */

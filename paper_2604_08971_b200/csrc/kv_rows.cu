@@ -466,9 +466,10 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
                             float top = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
 #pragma unroll
                             for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-                            top = fmaxf(top, m[nt][x]);
-                            keep[x] = top == m[nt][x] ? 1.0f : exp2_fast(m[nt][x] - top);
-                            m[nt][x] = top;
+                            // (each row for itself: what its neighbours hold changes no bit of it)
+                            const bool grew = top - m[nt][x] > 8.0f;
+                            keep[x] = grew ? exp2_fast(m[nt][x] - top) : 1.0f;
+                            m[nt][x] = grew ? top : m[nt][x];
                             l[nt][x] *= keep[x];
                         }
 #pragma unroll

@@ -303,8 +303,9 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                         ok = warp_wait(&misc->o_full[t], (n - 1) & 1, abort_flag);
                         if (!ok) break;
                         ptx::tc_fence_after_sync();
-                        const float keep = m == now ? 1.0f : exp2_fast((m - now) * c);
-                        m = now;
+                        // (each row for itself: what its neighbours hold changes no bit of it)
+                        const float keep = grew && m != now ? exp2_fast((m - now) * c) : 1.0f;
+                        if (grew) m = now;
                         l *= keep;
 #pragma unroll
                         for (int z = 0; z < D; z += 16) {

@@ -1,4 +1,6 @@
 """The serving calls (8-bit linear layer, cross attention, 8-bit cache) against their definitions in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -537,3 +539,155 @@ def test_serving_refusals(sn):
     assert sn.cross_attend_fwd(Q[:0], K[:0], K[:0]).shape == (0, 4, 1, 32)
     assert sn.cross_attend_fwd(Q[:, :, :0], K, K).shape == (2, 4, 0, 32)
     assert (sn.cache_attend_fwd(Q, kc, kc, s, s, table[:, :0], n) == 0).all() and sn.last_status() == 0
+
+
+# ------------------------------------------------------------------------------------------ where the paths inside could go wrong
+
+# (keys whose list of present ones is too long for a block's own; single rows, and rows packed into many tiles)
+LONG = [(2, 70, 5000, 4, 2, 64, 3, "both"), (3, 33, 4097, 2, 1, 128, 2, "interleaved"), (2, 3, 9000, 4, 2, 64, 4, "both"), (40, 1, 700, 8, 2, 32, 5, "both"),
+        (2, 32, 1030, 1, 1, 16, 1, "interleaved"), (2, 33, 1030, 1, 1, 16, 1, "interleaved"), (70, 1, 1000, 32, 1, 64, 32, "lengths"), (1, 1, 65, 64, 1, 128, 64, "all")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "x".join(map(str, c)))
+def test_cross_attend_long_lists(sn, case, dtype):
+    test_cross_attend(sn, case, dtype)
+
+
+def _ramps(Tq, N, d, top):
+    """q [Tq,d] and k [N,d] whose scores rise from -top to top along the keys for every other row, and fall for the rest."""
+    sign = np.where(np.arange(Tq) % 2, -1.0, 1.0)[:, None]
+    return np.ones((Tq, d)) * sign, np.linspace(-top, top, N)[:, None] / math.sqrt(d) * np.ones((N, d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("Tq,N,d", [(1, 900, 64), (8, 2000, 128), (20, 700, 32), (90, 1500, 64), (300, 1100, 128), (64, 130, 16)])
+@pytest.mark.parametrize("top", [15.0, 300.0])
+def test_rising_scores(sn, dtype, Tq, N, d, top):
+    """The running maximum moves with every step of the keys in one row and never again in the next one."""
+    q, k = _ramps(Tq, N, d, top)
+    g = torch.Generator().manual_seed(N)
+    Q = (torch.from_numpy(q) + 0.01 * torch.randn(q.shape, generator=g, dtype=torch.float64)).to(DT[dtype])[None, None]
+    K = torch.from_numpy(k).to(DT[dtype])[None, None]
+    V = torch.randn((1, 1, N, d), generator=g).to(DT[dtype])
+    O = sn.cross_attend_fwd(Q.cuda(), K.cuda(), V.cuda())
+    _check_attention(O, Q, None, 1, lambda b, h: (_np(K[0, 0]), _np(V[0, 0]), np.ones((Tq, N), bool)), DT[dtype], WEIGHTS[dtype])
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("Tq,N,d,page", [(1, 900, 64, 64), (8, 2000, 128, 16), (40, 333, 32, 128)])
+def test_rising_scores_cache(sn, fmt, dtype, Tq, N, d, page):
+    q, k = _ramps(Tq, N, d, 40.0)
+    rng = np.random.default_rng(N)
+    cols = -(-N // page)
+    kc, ks = np.zeros((cols, 1, page, d), np.int8 if fmt == "i8" else np.uint8), np.zeros((cols, 1), np.float32)
+    vc, vs = _pool(rng, cols, 1, page, d, fmt)
+    table = np.arange(cols, dtype=np.int32)[None]
+    ref.append(k[None, None], kc, ks, table, np.zeros(1, np.int32), np.ones((1, N), bool), fmt)
+    Q = torch.from_numpy(q).to(DT[dtype])[None, None]
+    O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, np.array([N], np.int32)))
+    kk, vv = ((ref.values(c, fmt) * s[..., None, None]).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
+    _check_attention(O, Q, None, 1, lambda b, h: (kk, vv, np.ones((Tq, N), bool)), DT[dtype], 2.0 ** -11 if dtype != "f32" else 0.0, q16=dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("Tq", [1, 6, 130])
+def test_what_is_no_number_stays_where_it_is(sn, dtype, Tq):
+    """A NaN in a query makes its own rows NaN, one in a present key or value those of its sample and group, and no other bit changes."""
+    B, Tk, Hq, Hk, d = 3, 300, 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(12)
+    Q, K, V = (torch.randn((B, h, t, d), generator=g, device="cuda").to(DT[dtype]) for h, t in ((Hq, Tq), (Hk, Tk), (Hk, Tk)))
+    clean = sn.cross_attend_fwd(Q, K, V)
+    want = torch.zeros((B, Hq, Tq), dtype=torch.bool, device="cuda")
+    Q[0, 1, Tq // 2, 5] = float("nan")
+    want[0, 1, Tq // 2] = True
+    K[1, 0, 271, 63] = float("nan")
+    want[1, :2] = True
+    V[2, 1, 3] = float("nan")
+    want[2, 2:] = True
+    O = sn.cross_attend_fwd(Q, K, V)
+    assert torch.equal(torch.isnan(O).all(-1), want) and torch.equal(torch.isnan(O).any(-1), want)
+    assert torch.equal(O[~want], clean[~want]) and sn.last_status() == 0
+
+
+def _cache_call(B, Tq, cols, page, Hq, Hk, d, seed):
+    rng = np.random.default_rng(seed)
+    (kc, ks), (vc, vs) = (_pool(rng, 97, Hk, page, d, "i8") for _ in range(2))
+    table = rng.integers(0, 97, (B, cols)).astype(np.int32)         # pages that several samples, and several places, share
+    lengths = rng.integers(0, cols * page + 1, B).astype(np.int32)
+    Q = torch.randn((B, Hq, Tq, d), generator=torch.Generator().manual_seed(seed)).bfloat16()
+    return [Q.cuda()] + _cuda((kc // 8).astype(np.int8), vc, ks, vs, table, lengths)
+
+
+# (samples enough that the last block of a group joins its parts, and so few that a launch of its own does)
+SHARED = [(32, 1, 30, 32, 4, 2, 64), (3, 1, 300, 16, 8, 1, 128), (130, 1, 40, 64, 4, 1, 32), (9, 5, 64, 128, 16, 4, 128), (1, 2, 500, 32, 4, 4, 16), (5, 1, 7, 16, 4, 2, 32)]
+
+
+def test_calls_in_turn_on_streams(sn):
+    """Calls of different shapes in turn on one context and a stream of its own, then from two contexts on two streams at once: every result is
+    the one that the call gives alone, and that of fp32 rows within both results' tolerance."""
+    calls = [_cache_call(*s, seed=i) for i, s in enumerate(SHARED)]
+    alone = [sn.cache_attend_fwd(*c) for c in calls]
+    for c, o in zip(calls, alone):
+        Q, kc, vc, ks, vs, table, lengths = [x.cpu() for x in c]
+        Hk, page, d = kc.shape[1:]
+        per, cap = Q.shape[1] // Hk, table.shape[1] * page
+
+        def keys_of(b, g):
+            n = int(lengths[b])
+            k, v = ((x.double() * s.double()[..., None, None])[table[b].long()][:, g].reshape(cap, d)[:n].numpy() for x, s in ((kc, ks), (vc, vs)))
+            return k, v, np.ones((Q.shape[2], n), bool)
+        _check_attention(o, Q, None, per, keys_of, torch.bfloat16, 2.0 ** -11, q16=True)
+    torch.cuda.synchronize()
+    other = sentry.Sentry(0)
+    try:
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        got = []
+        for i in range(40):
+            with torch.cuda.stream(one):
+                got.append((i % 6, sn.cache_attend_fwd(*calls[i % 6])))
+            with torch.cuda.stream(two):
+                got.append((5 - i % 6, other.cache_attend_fwd(*calls[5 - i % 6])))
+        torch.cuda.synchronize()
+        for i, o in got:
+            assert torch.equal(o, alone[i]), i
+        assert sn.last_status() == 0 and other.last_status() == 0
+    finally:
+        other.close()
+
+
+def test_many_rows_on_two_streams(sn):
+    """Kernels that hold tensor memory (projection, many rows of cross attention) from two contexts on two streams at once."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    X = torch.randn((1500, 256), generator=g, device="cuda").bfloat16()
+    w, ws = sn.quantize_rows_i8(torch.randn((768, 256), generator=g, device="cuda"))
+    Q, K, V = (torch.randn((4, h, t, 64), generator=g, device="cuda").bfloat16() for h, t in ((8, 300), (2, 900), (2, 900)))
+    run = lambda s: (s.linear_i8(*s.quantize_rows_i8(X), w, ws), s.cross_attend_fwd(Q, K, V))
+    want = run(sn)
+    torch.cuda.synchronize()
+    other = sentry.Sentry(0)
+    try:
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        got = []
+        for _ in range(10):
+            for s, st in zip((sn, other), streams):
+                with torch.cuda.stream(st):
+                    got.append(run(s))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for o in got for a, b in zip(o, want))
+    finally:
+        other.close()
+
+
+def test_sizes_of_one(sn):
+    """Views whose dimensions of size one have strides of their own, and one token of a long tensor."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    Q, K, V = (torch.randn((5, h, t, 32), generator=g, device="cuda").bfloat16() for h, t in ((2, 9), (1, 40), (1, 40)))
+    for i in (0, 8):
+        for n in (1, 40):
+            q, k, v = Q[3:4, :, i:i + 1], K[3:4, :, :n], V[3:4, :, 40 - n:]
+            assert torch.equal(sn.cross_attend_fwd(q, k, v), sn.cross_attend_fwd(q.contiguous(), k.contiguous(), v.contiguous()))
+    odd = torch.randn(8 * 32 + 7, generator=g, device="cuda").bfloat16()
+    q = torch.as_strided(odd, (1, 8, 1, 32), (3, 32, 5, 1))          # (no index ever multiplies the 3 and the 5)
+    assert torch.equal(sn.cross_attend_fwd(q, K[:1], V[:1]), sn.cross_attend_fwd(q.clone(memory_format=torch.contiguous_format), K[:1], V[:1]))

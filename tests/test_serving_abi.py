@@ -65,6 +65,8 @@ def test_cross_refusals(lib, ctx):
     for kw in (dict(d=48), dict(Hq=512, Hk=2), dict(Tq=1 << 24), dict(Tk=1 << 24), dict(B=1 << 23)):
         assert f(_cross(**kw)) == UNSUPPORTED, kw
     assert f(_cross(q_stride=(96, 4, 32))) == UNSUPPORTED and f(_cross(k_stride=(-8, 8, 8))) == SHAPE
+    assert f(_cross(k_stride=(8, 32, 0))) == UNSUPPORTED and f(_cross(v_stride=(8, 32, 0))) == UNSUPPORTED   # one key for all
+    assert f(_cross(q_stride=((1 << 38) + 8, 32, 32))) == UNSUPPORTED
     assert f(_cross(k_h=3), kept=None) == SHAPE                        # every head, but fewer outputs
     assert f(_cross(), ids=P) == INVALID and f(_cross(), masks=P) == INVALID
     for bad in ("q", "k", "v", "o"):
@@ -83,7 +85,7 @@ def _cache(**kw):
 
 
 BAD_CACHES = [(dict(format=sentry.SENTRY_BF16), INVALID), (dict(Hk=0), SHAPE), (dict(n_pages=-1), SHAPE), (dict(max_pages=-1), SHAPE),
-              (dict(d=8), UNSUPPORTED), (dict(page=48), UNSUPPORTED), (dict(max_pages=1 << 28, page=16), UNSUPPORTED),
+              (dict(d=8), UNSUPPORTED), (dict(page=48), UNSUPPORTED), (dict(max_pages=1 << 28, page=16), UNSUPPORTED), (dict(n_pages=1 << 27), UNSUPPORTED),
               (dict(k=None), INVALID), (dict(v=P + 8), INVALID), (dict(k_scales=None), INVALID), (dict(page_table=P + 1), INVALID)]
 
 
