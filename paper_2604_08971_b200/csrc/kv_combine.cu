@@ -1,36 +1,30 @@
-// Joins the parts of attention whose axis of keys was split over blocks.
+// Joins the parts of cross attention of many rows whose axis of keys was split over blocks.
 #include "kv_attend.cuh"
 
 namespace {
 
 constexpr int kCombineThreads = 256;
-constexpr int kMaxParts = 1024;     // of a row: at most the blocks of a wave
+constexpr int kMaxParts = 64;       // of a row
 
 // A block per row: its warps take the parts in turn, with the loads of several on the way, and meet in shared memory.  (A warp per row, part
 // after part: 37 us for 16 rows of 128 parts.)
 template <bool BF16>
-__global__ void __launch_bounds__(kCombineThreads) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, const int2* __restrict__ plan,
-                                                         int n_splits) {
+__global__ void __launch_bounds__(kCombineThreads) kv_combine_kernel(const KvAttendArgs a, const float* __restrict__ part, const float2* __restrict__ ml, int n) {
     __shared__ float s_weight[kMaxParts], s_acc[kCombineThreads / 32][128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const size_t row = blockIdx.x, each = (size_t)a.k_h * a.Tq;      // rows of a sample
     grid_dependency_wait();
     const int b = (int)(row / each);
     const size_t in = row - (size_t)b * each;
-    const int2 mine = plan != nullptr ? plan[b] : make_int2(b * n_splits, n_splits);
-    const int n = min(mine.y, kMaxParts);
-    if (plan != nullptr && n == 1) return;              // (written where it was computed)
     if (kv_head(a, b, (int)(in / a.Tq)) < 0) return;    // (its zero rows are written)
     // every warp by itself: the maximum, the total, and the weights of all parts
-    const float2* x0 = ml + (size_t)mine.x * each + in;
-    // (the loads of 128 parts at a time, all on the way together)
+    const float2* x0 = ml + (size_t)b * n * each + in;
     float top = -INFINITY, total = 0.0f;
-    float2 x[4];
+    float2 x[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < n ? x0[(i * 32 + lane) * each] : make_float2(-INFINITY, 0.0f);
+    for (int i = 0; i < 2; ++i) x[i] = i * 32 + lane < n ? x0[(i * 32 + lane) * each] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, x[i].x);
-    for (int s = 128 + lane; s < n; s += 32) top = fmaxf(top, x0[s * each].x);
+    for (int i = 0; i < 2; ++i) top = fmaxf(top, x[i].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float ref = top == -INFINITY ? 0.0f : top;
@@ -41,9 +35,8 @@ __global__ void __launch_bounds__(kCombineThreads) kv_combine_kernel(const KvAtt
         if (warp == 0) s_weight[s] = v.x == -INFINITY && v.y == 0.0f ? -1.0f : f;
     };
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
         if (i * 32 + lane < n) take(i * 32 + lane, x[i]);
-    for (int s = 128 + lane; s < n; s += 32) take(s, x0[s * each]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     __syncthreads();
@@ -54,7 +47,7 @@ __global__ void __launch_bounds__(kCombineThreads) kv_combine_kernel(const KvAtt
     for (int s = warp * subs + sub; s < n; s += kCombineThreads / 32 * subs) {
         const float f = s_weight[s];
         if (f < 0.0f) continue;
-        const float4 v = *reinterpret_cast<const float4*>(part + ((mine.x + s) * each + in) * a.d + c * 4);
+        const float4 v = *reinterpret_cast<const float4*>(part + (((size_t)b * n + s) * each + in) * a.d + c * 4);
         acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
     }
     for (int o = lanes; o < 32; o <<= 1) {
@@ -77,10 +70,10 @@ __global__ void __launch_bounds__(kCombineThreads) kv_combine_kernel(const KvAtt
 
 }  // namespace
 
-int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, const int2* plan, int n_splits, cudaStream_t st) {
+int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, int n_splits, cudaStream_t st) {
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     LaunchScope ls(ctx, KS_KV_COMBINE, st);
     auto k = a.dtype == SENTRY_BF16 ? kv_combine_kernel<true> : kv_combine_kernel<false>;
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)rows), dim3(kCombineThreads), 0, st, a, part, ml, plan, n_splits));
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)rows), dim3(kCombineThreads), 0, st, a, part, ml, n_splits));
     return SENTRY_OK;
 }

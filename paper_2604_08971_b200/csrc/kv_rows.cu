@@ -3,7 +3,7 @@
 // The rows of one KV group (kept heads x Tq) share its keys, so they are packed into tiles of 8 or 16 rows, and a block takes a tile and a
 // stretch of the keys.  One warp brings tiles of 32 keys into a ring by TMA, which also swizzles them against bank conflicts; four others
 // take them in turn, each with a running maximum and sum of its own (log2 domain) and both products on the warp MMA: no barrier between
-// them until the four partial results meet.  Long axes are shared out over blocks; kv_combine_kernel joins the parts.
+// them until the four partial results meet.  Long axes are shared out over blocks; the last to finish joins the parts.
 // The keys are the MMA's 16 rows and the queries its 8 columns (S^T = K Q^T, O^T = V^T P^T): a decoder's few rows fill it, where queries as
 // rows left half of it and half of the exponentials empty.
 // What bounds it: the bytes of K and V, read once from memory, and the instructions that turn codes into operands.  They go from
@@ -110,19 +110,14 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // Which stretch of which sample's keys a block takes.  The samples' lengths differ and only the device knows them, so that every block works
 // out the same shares: as many blocks to a sample as it has stretches of `chunk` tiles (one at least), so that all fit one wave.
 struct RowsShare { int b, split, n, first, len; };   // first: number of the sample's first part among all samples' parts; len: its keys
-constexpr int kFusedParts = 16;
-__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room, bool fused) {
+__device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room) {
     const int lane = threadIdx.x & 31;
     auto length_of = [&](int b) { return b < a.B ? kv_length(a, b) : 0; };
     auto tiles = [](int len) { return (len + kKeys - 1) / kKeys; };
     const int mine = length_of(lane);
-    int sum = tiles(mine), top = sum;
+    int sum = tiles(mine);
 #pragma unroll 4
-    for (int b0 = 32; b0 < a.B; b0 += 32) {
-        const int t = tiles(length_of(b0 + lane));
-        sum += t;
-        top = max(top, t);
-    }
+    for (int b0 = 32; b0 < a.B; b0 += 32) sum += tiles(length_of(b0 + lane));
     const long long total = (long long)__reduce_add_sync(0xffffffffu, sum >> 8) * 256 + __reduce_add_sync(0xffffffffu, sum & 255);
     int chunk = max((int)((total + room - 1) / room), kWarps);
     if (a.B <= 32) {
@@ -135,7 +130,6 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
             else low = mid + 1;
         }
     }
-    if (fused) chunk = max(chunk, (__reduce_max_sync(0xffffffffu, top) + kFusedParts - 1) / kFusedParts);
     RowsShare r = {-1, 0, 0, 0, 0};
     int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -161,13 +155,55 @@ __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit,
     return r;
 }
 
-// room: 0: a block per group and row tile takes all of its keys.  Otherwise the keys are shared out (rows_share), part: [parts][k_h][Tq][D] sums,
-// ml: [parts][k_h][Tq] (maximum, total).  The parts of a group's rows are joined by the last of its blocks (counters: one for each group and row
-// tile, left at zero), or, where a sample may have many, by kv_combine_kernel, for which plan: [B] says (first part, parts).
+// Where the parts of split axes meet.  part: [parts][k_h][Tq][D] sums, ml: [parts][k_h][Tq] (maximum, total).  The last block of every
+// kJoin neighbouring parts of a group's row tile joins those into one of `part2`, the last of these joins the results; kJoin parts at most
+// go straight to the second step.  (A launch of its own for it costs 6 us behind the blocks' end, and one block alone is slow with a hundred parts.)
+// counters: one of every group's row tile, then one of every kJoin parts of it; left at zero.
+constexpr int kJoin = 16;
+struct RowsJoin {
+    float *part, *part2;
+    float2 *ml, *ml2;
+    unsigned int* counters;
+    int room;                  // parts beside the first of every sample; 0: no axis is split, a block per group and row tile takes all keys
+};
+
+// Four columns of n parts of a row, `each` rows apart, and their (maximum, total).  Not inlined: what it holds of kJoin / 2 parts at a time
+// would cost the loop over the keys its registers.
+template <int D>
+__device__ __noinline__ float4 join_parts(const float* part, const float2* ml, size_t each, int n, float2& out) {
+    constexpr int S = kJoin / 2;
+    float top = -INFINITY, sum = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s0 = 0; s0 < n; s0 += S, part += S * each * D, ml += S * each) {
+        float2 x[S];
+        float4 p[S];
+        float now = top;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const bool in = s0 + s < n;
+            x[s] = in ? __ldcg(ml + s * each) : make_float2(-INFINITY, 0.0f);
+            p[s] = in ? __ldcg(reinterpret_cast<const float4*>(part + s * each * D)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) now = fmaxf(now, x[s].x);
+        const float ref = now == -INFINITY ? 0.0f : now, keep = top == now ? 1.0f : exp2_fast(top - ref);
+        top = now;
+        sum *= keep;
+        v.x *= keep; v.y *= keep; v.z *= keep; v.w *= keep;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const float f = exp2_fast(x[s].x - ref);
+            sum += x[s].y * f;
+            v.x += p[s].x * f; v.y += p[s].y * f; v.z += p[s].z * f; v.w += p[s].w * f;
+        }
+    }
+    out = make_float2(top, sum);
+    return v;
+}
+
 template <int KV, int D, bool BF16, int NT>
 __global__ void __launch_bounds__(kRowsThreads, RowsCfg<KV, D>::BLOCKS - (NT > 1 && RowsCfg<KV, D>::BLOCKS > 2))
-kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float* __restrict__ part, float2* __restrict__ ml, int2* __restrict__ plan, unsigned int* __restrict__ counters,
-               int room) {
+kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const RowsJoin meet) {
     using C = RowsCfg<KV, D>;
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
@@ -193,19 +229,16 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
         s_abort = 0;
         ptx::fence_barrier_init();
     }
-    // those who join the parts are few and small: their launch need not wait for this one's end
-    if (plan != nullptr && (long long)a.B * a.k_h * a.Tq <= 1024) grid_dependents_start();
-    else grid_dependents_start_if_small();
+    grid_dependents_start_if_small();
     grid_dependency_wait();
     RowsShare share = {(int)blockIdx.x / a.Hk, 0, 1, 0, 0};
-    if (room > 0) share = rows_share(a, blockIdx.x / a.Hk, room, counters != nullptr);       // (every warp for itself)
+    if (meet.room > 0) share = rows_share(a, blockIdx.x / a.Hk, meet.room);       // (every warp for itself)
     else share.len = kv_length(a, share.b);
     if (share.b < 0) return;
     const int b = share.b;
     if (warp == 0) {
         const int n = kv_group_heads(a, b, g, g == 0 && share.split == 0 && blockIdx.y == 0, s_head, s_pos);
         if (lane == 0) s_heads = n;
-        if (plan != nullptr && lane == 0 && share.split == 0 && g == 0 && blockIdx.y == 0) plan[b] = make_int2(share.first, share.n);
     }
     const int len = share.len;
     const int tiles = (len + kKeys - 1) / kKeys;
@@ -641,50 +674,57 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, float*
                 reinterpret_cast<uint32_t*>(a.O)[(out * D + c) / 2] = pack2<BF16>(sum == 0.0f ? 0.0f : x * inv, sum == 0.0f ? 0.0f : y * inv);
             } else {
                 const size_t at = (size_t)(share.first + share.split) * a.k_h * a.Tq + in;
-                *reinterpret_cast<float2*>(part + at * D + c) = make_float2(x, y);
-                if (c == 0) ml[at] = make_float2(top, sum);
+                *reinterpret_cast<float2*>(meet.part + at * D + c) = make_float2(x, y);
+                if (c == 0) meet.ml[at] = make_float2(top, sum);
             }
         }
         ptx::fence_proxy_async_smem();          // the next rows' copies come where these parts lay
         __syncthreads();
         if (*abort_flag) break;
     }
-    if (counters != nullptr && share.n > 1) {
-        // the last block of the group and row tile to come here joins the parts
-        __threadfence();
-        __syncthreads();
-        unsigned int* counter = counters + ((size_t)b * a.Hk + g) * gridDim.y + blockIdx.y;
-        if (threadIdx.x == 0) s_heads = atomicAdd(counter, 1u) == (unsigned)share.n - 1u;
-        __syncthreads();
-        if (s_heads) {
+    if (share.n > 1) {
+        const size_t each = (size_t)a.k_h * a.Tq;
+        auto is_last = [&](unsigned int* counter, int of) {
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) s_heads = atomicAdd(counter, 1u) == (unsigned)of - 1u;
+            __syncthreads();
+            if (!s_heads) return false;
             __threadfence();
             if (threadIdx.x == 0) *counter = 0u;
-            const size_t each = (size_t)a.k_h * a.Tq;
+            return true;
+        };
+        // n parts from part `first` on, into part `to` of the second step, or (to < 0) into the result
+        auto join = [&](const float* part, const float2* ml, size_t first, int n, long long to) {
             for (int row0 = blockIdx.y * ROWS; row0 < rows; row0 += gridDim.y * ROWS)
                 for (int e = threadIdx.x; e < min(ROWS, rows - row0) * (D / 4); e += kRowsThreads) {
                     const int row = row0 + e / (D / 4), c = e % (D / 4) * 4;
-                    const size_t in = (size_t)s_pos[row / a.Tq] * a.Tq + row % a.Tq, first = (size_t)share.first * each + in;
-                    float top = -INFINITY, sum = 0.0f;
-                    float2 x[kFusedParts];
-#pragma unroll
-                    for (int s = 0; s < kFusedParts; ++s) {
-                        x[s] = s < share.n ? __ldcg(ml + first + s * each) : make_float2(-INFINITY, 0.0f);
-                        top = fmaxf(top, x[s].x);
+                    const size_t in = (size_t)s_pos[row / a.Tq] * a.Tq + row % a.Tq, from = first * each + in;
+                    float2 x;
+                    const float4 v = join_parts<D>(part + from * D + c, ml + from, each, n, x);
+                    if (to >= 0) {
+                        const size_t at = (size_t)to * each + in;
+                        *reinterpret_cast<float4*>(meet.part2 + at * D + c) = v;
+                        if (c == 0) meet.ml2[at] = x;
+                    } else {
+                        const float inv = x.y == 0.0f ? 0.0f : 1.0f / x.y;
+                        *reinterpret_cast<uint2*>((uint16_t*)a.O + ((size_t)b * each + in) * D + c) =
+                            x.y == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack2<BF16>(v.x * inv, v.y * inv), pack2<BF16>(v.z * inv, v.w * inv));
                     }
-                    const float ref = top == -INFINITY ? 0.0f : top;
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                    for (int s = 0; s < kFusedParts; ++s) {
-                        if (s >= share.n) break;
-                        const float f = exp2_fast(x[s].x - ref);
-                        const float4 p = __ldcg(reinterpret_cast<const float4*>(part + (first + s * each) * D + c));
-                        sum += x[s].y * f;
-                        v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
-                    }
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    if (sum == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    *reinterpret_cast<uint2*>((uint16_t*)a.O + ((size_t)b * each + in) * D + c) = make_uint2(pack2<BF16>(v.x * inv, v.y * inv), pack2<BF16>(v.z * inv, v.w * inv));
                 }
+        };
+        unsigned int* own = meet.counters + ((size_t)b * a.Hk + g) * gridDim.y + blockIdx.y;
+        if (share.n <= kJoin) {
+            if (is_last(own, share.n)) join(meet.part, meet.ml, share.first, share.n, -1);
+        } else {
+            // (a sample's results of the first step lie behind those of the samples before: that many are enough for all)
+            const int sets = (share.n + kJoin - 1) / kJoin, set = share.split / kJoin, to = share.first / kJoin + b;
+            unsigned int* counter = meet.counters + ((size_t)(a.B + to + set) * a.Hk + g) * gridDim.y + blockIdx.y;
+            const int n = min(kJoin, share.n - set * kJoin);
+            if (is_last(counter, n)) {
+                join(meet.part, meet.ml, share.first + set * kJoin, n, to + set);
+                if (is_last(own, sets)) join(meet.part2, meet.ml2, to, sets, -1);
+            }
         }
     }
     if (*abort_flag) {
@@ -712,25 +752,24 @@ int rows_wave(const KvAttendArgs& a) {
     return a.B < wave / a.Hk && a.Tk > kWarps * kKeys ? (int)wave : 0;
 }
 
-// Whether the last block of a group joins its parts: where the samples are enough that kFusedParts of each fill the wave.  (A launch of its own
-// costs 4 us behind the blocks' end; but one block is slow with a hundred parts.)
-bool rows_fused(const KvAttendArgs& a, int wave) {
-    return wave > 0 && (long long)a.B * kFusedParts >= wave / a.Hk && (long long)a.B * a.Hk * rows_tiles(a) <= kCounters;
-}
+// Parts of the second step of the joining: those of all samples, a last one with fewer than kJoin for each.
+// (2 B + parts / kJoin counters of every group's row tile, and B of those are less than a wave's blocks.)
+static_assert(2 * 4 * kSmCount + 4 * kSmCount / kJoin <= kCounters, "counters");
+size_t rows_parts2(const KvAttendArgs& a, int wave) { return (size_t)(wave / a.Hk / kJoin + a.B); }
 
 template <int KV, int D, bool BF16, int NT>
 int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     using C = RowsCfg<KV, D>;
-    const int wave = rows_wave(a), room = wave / a.Hk - a.B;      // parts beside the first of every sample
-    const bool fused = rows_fused(a, wave);
-    const size_t rows = (size_t)a.k_h * a.Tq;
-    float* part = nullptr;
-    float2* ml = nullptr;
-    int2* plan = nullptr;
+    const int wave = rows_wave(a);
+    RowsJoin meet = {};
     if (wave > 0) {
-        part = ws.take<float>(wave / a.Hk * rows * D);
-        ml = ws.take<float2>(wave / a.Hk * rows);
-        if (!fused) plan = ws.take<int2>(a.B);
+        const size_t rows = (size_t)a.k_h * a.Tq;
+        meet.part = ws.take<float>(wave / a.Hk * rows * D);
+        meet.ml = ws.take<float2>(wave / a.Hk * rows);
+        meet.part2 = ws.take<float>(rows_parts2(a, wave) * rows * D);
+        meet.ml2 = ws.take<float2>(rows_parts2(a, wave) * rows);
+        meet.counters = ctx->d_counters;
+        meet.room = wave / a.Hk - a.B;
         if (!ws.ok) return SENTRY_ERR_WORKSPACE;
     }
     KvMaps maps = {};
@@ -742,10 +781,9 @@ int launch_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
         LaunchScope ls(ctx, KS_KV_ATTEND, st);
-        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kRowsThreads), C::SMEM, st, maps, a, part, ml,
-                                       plan, fused ? ctx->d_counters : nullptr, wave > 0 ? room : 0));
+        SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(wave > 0 ? wave / a.Hk * a.Hk : a.B * a.Hk), (unsigned)rows_tiles(a)), dim3(kRowsThreads), C::SMEM, st, maps, a, meet));
     }
-    return plan != nullptr ? launch_kv_combine(ctx, a, part, ml, plan, 0, st) : SENTRY_OK;
+    return SENTRY_OK;
 }
 
 template <int KV, int D, bool BF16>
@@ -768,8 +806,11 @@ int launch_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t s
 size_t kv_rows_ws_bytes(const KvAttendArgs& a) {
     const int wave = rows_wave(a);
     if (wave == 0) return 0;
-    const size_t parts = wave / a.Hk, rows = (size_t)a.k_h * a.Tq;
-    return align_up(parts * rows * a.d * sizeof(float), 256) + align_up(parts * rows * sizeof(float2), 256) + a.B * sizeof(int2) + 512;
+    const size_t rows = (size_t)a.k_h * a.Tq;
+    size_t bytes = 512;
+    for (const size_t parts : {(size_t)(wave / a.Hk), rows_parts2(a, wave)})
+        bytes += align_up(parts * rows * a.d * sizeof(float), 256) + align_up(parts * rows * sizeof(float2), 256);
+    return bytes;
 }
 
 int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {

@@ -474,7 +474,7 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
         SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((long long)a.B * a.Hk * n_splits), (unsigned)row_blocks(a)), dim3(C::THREADS), C::SMEM, st, maps, a, (const int32_t*)list,
                                        (const int32_t*)counts, part, ml, n_splits));
     }
-    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, nullptr, n_splits, st) : SENTRY_OK;
+    return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
 }
 
 template <bool BF16>

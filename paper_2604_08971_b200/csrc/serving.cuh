@@ -37,7 +37,7 @@ size_t kv_rows_ws_bytes(const KvAttendArgs& a);
 bool kv_tc_takes(const KvAttendArgs& a);                                                   // 16-bit dense, many rows
 size_t kv_tc_ws_bytes(const KvAttendArgs& a);
 int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);
-int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, const int2* plan, int n_splits, cudaStream_t st);
+int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, int n_splits, cudaStream_t st);
 int launch_kv_rows(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);   // 16-bit rows, few of them
 
 struct AppendArgs {
