@@ -12,6 +12,9 @@
 // words are interleaved byte by byte.  The weights get from the first product's layout to the second's by a transposition of 8 x 8
 // matrices among registers.  8-bit codes become fp16 exactly; a page's key scale multiplies the scores, its value scale the weights.
 // The maximum is followed only where a score exceeds it by 2^8.
+// One token of 32 samples of up to 4096 e4m3 tokens (16 heads on 4, d 128, 87 MB): 24 us, 3.6 TB/s over all; a block's first keys arrive 3.5 us
+// after its start (lengths, page, keys: three loads that depend on one another), between that and the last tile the loads run at 5 to 5.7 TB/s,
+// and the parts meet in 3.  i8 of d 64 (2 x 131072 tokens, 67 MB): 29 us, where issue is as long as the bytes (640 instructions a warp for 32 keys).
 // Every wait is bounded; on expiry the block raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"

@@ -15,7 +15,8 @@ namespace {
 // ------------------------------------------------------------------------------------------------ quantise rows
 // WARPS warps share a row (1: eight rows a block; 8: one row a block).  Up to HELD pieces of 16 bytes a lane stay in registers between the
 // two steps; what a longer row has beyond them is read a second time.  Bound by the bytes, as long as a value costs few instructions:
-// the maximum runs on pairs of magnitude bits, and the quotient is rounded by an addition, two at a time (codes_i8).
+// the maximum runs on pairs of magnitude bits, and the quotient is rounded by an addition, two at a time (codes_i8): 65536 x 1024 bf16
+// in 31.5 us, 6.4 TB/s, what a copy reaches.
 template <typename T, int WARPS, int HELD>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ X, int8_t* __restrict__ codes, float* __restrict__ scales,
                                                             int M, int K) {
@@ -172,7 +173,8 @@ __host__ __device__ constexpr uint32_t umma_idesc_i8(int M, int N) {
 
 // A tile: 128 P tokens x BN channels, K in steps of 128 bytes; a pair's CTAs have 128 tokens and half of the channels' weights each, so that
 // a tile costs the L2 and shared memory two thirds of what two single CTAs' would.  Two accumulators in tensor memory: the eight
-// epilogue warps scale one and store it, by TMA, while the other is summed.
+// epilogue warps scale one and store it, by TMA, while the other is summed.  Bound by the tensor pipe (74 % of its cycles) and the 268 MB
+// of results beside it: 2.5 PFLOP/s of 8-bit products.
 // Tried without gain at 65536 x 1024 x 2048 (108 us): the accumulator handed over before it is scaled (115), sixteen epilogue warps
 // (114), six stages and stores of 32 bytes a row (125), a pair's weights kept in shared memory with three stages of X (141).
 constexpr int kLinThreads = 384, kLinEpiWarp0 = 4, kLinEpiWarps = 8;
