@@ -63,3 +63,33 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(hi), "f"(lo));
     return v;
 }
+// two codes in the low 16 bits of w -> fp16 pair
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_hi_to_f16x2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+// bytes (already + 128) -> fp16: 0x6400 | u is 1024 + u, exactly
+__device__ __forceinline__ uint32_t biased_to_f16x2(uint32_t pair) {
+    const uint32_t bias = 0x64806480u;   // 1152
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(bias));
+    return r;
+}
+// four codes of a word, in order, as two fp16 pairs
+template <bool I8>
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& p01, uint32_t& p23) {
+    if constexpr (I8) {
+        const uint32_t u = w ^ 0x80808080u;
+        p01 = biased_to_f16x2(__byte_perm(u, 0x64646464u, 0x4140));
+        p23 = biased_to_f16x2(__byte_perm(u, 0x64646464u, 0x4342));
+    } else {
+        p01 = e4m3x2_to_f16x2(w);
+        p23 = e4m3x2_hi_to_f16x2(w);
+    }
+}

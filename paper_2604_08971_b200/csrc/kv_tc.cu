@@ -1,4 +1,4 @@
-// Cross attention of many rows on the 5th-generation tensor cores (16-bit types).
+// Attention of many rows on the 5th-generation tensor cores (16-bit rows; dense 16-bit keys, or the 8-bit cache).
 //
 // The rows of a KV group (kept heads x Tq) are packed; a CTA takes two tiles of 128 of them and walks the present keys, KN at a time:
 //   S_t = Q_t K^T        tcgen05, both operands in shared memory (128-byte rows, swizzled), S in tensor memory
@@ -14,8 +14,10 @@
 // 910 with one CTA and 128 keys; 32 samples of 211 rows on 648 keys, 7 of 12 heads on 4: 28 us against 32); at d 128 tensor memory has room for
 // one, whose steps are of 128 keys (the same rows at d 128: 917 us in a burst, 1.2 PFLOP/s; 1050 under the power limit).  Registers hold all but the
 // last 32 scores of a step from the maximum to the weights: those are read twice (all of them at d 128: 945 us, with spills).
-// K and V come by TMA where the present keys of a step follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
+// Dense K and V come by TMA where the present keys of a step follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
 // where they do not: the last tile of a sample, and tiles across the border of a missing modality.
+// A cache's codes are made fp16 by the loading warps, exactly; Q and the weights meet them as fp16.  A page's key scale multiplies its scores, and the
+// logarithm of its value scale is added to them, so that the weights carry it and O needs no unit of its own; the sum takes it out again.
 // Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"
@@ -32,11 +34,12 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {     // no
     return r;
 }
 
-template <int D>
+template <int D, bool CODES>
 struct TcCfg {
     static constexpr int KN = D <= 64 ? 64 : 128;            // keys of a step
     static constexpr int CTAS = KN == 64 ? 2 : 1;            // of an SM
-    static constexpr int LOAD_WARPS = KN == 64 ? 1 : 3;      // after the four softmax warps of each tile; then one issuer
+    // after the four softmax warps of each tile; then one issuer.  (Who makes 16 bits of codes has more to do than who waits for copies.)
+    static constexpr int LOAD_WARPS = CODES ? (KN == 64 ? 3 : 7) : KN == 64 ? 1 : 3;
     static constexpr int LOAD_WARP0 = 8, ISSUE_WARP = LOAD_WARP0 + LOAD_WARPS, THREADS = (ISSUE_WARP + 1) * 32;
     static constexpr int TMEM = 512 / CTAS, O_COL = 2 * KN;  // tensor memory: S of both tiles, then O of both
     static constexpr int RB = D >= 64 ? 128 : D * 2;         // bytes of a shared-memory row (64 elements at most)
@@ -44,19 +47,28 @@ struct TcCfg {
     static constexpr int SLAB = kTM * RB, TILE = SLABS * SLAB;         // of Q: 128 rows of D elements
     static constexpr int KSLAB = KN * RB, KTILE = SLABS * KSLAB;       // of K and V
     static constexpr int STAGES = D == 128 ? 2 : 4;          // of K, and of V
-    static constexpr int HELD = KN == 64 ? 1 : 3;            // blocks of 32 scores that a thread keeps from the maximum to the weights
+    static constexpr int HELD = CODES ? 0 : KN == 64 ? 1 : 3;  // blocks of 32 scores that a thread keeps from the maximum to the weights
+    static constexpr int META = 2 * STAGES;                  // steps whose pages' scales are kept: what a reader of one needs lies at most STAGES ahead
     static constexpr int SMEM = 2 * TILE + 2 * STAGES * KTILE + 1024;
     static_assert(O_COL + 2 * D <= TMEM && (KN == 128 || SLABS == 1), "tensor memory, and slabs of 128 rows");
 };
 struct TcMisc {
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2], p_full[2], o_full[2], meta_full[8];
     uint32_t tmem_base;
     int abort_flag;
     int n_heads;
     short head[kServeMaxHeads], pos[kServeMaxHeads];
     int red[66];
-    uint16_t list[kTcListed];
+    union {
+        uint16_t list[kTcListed];
+        struct {                            // of a cache
+            float4 meta[8][8];              // of every 16 keys of a step: key scale, log2 of the value scale in units of vref, its inverse, -
+            unsigned holes[8];              // which of them are not there
+            float q_scale[2 * kTM];
+            unsigned top[16];
+        } c;
+    };
 };
 
 // 16-byte piece c of row r in a tile of rows of RB bytes, swizzled in that row width's mode
@@ -67,12 +79,14 @@ __device__ __forceinline__ uint32_t tile_offset(int r, int c) {
     return (uint32_t)((c / PER) * (128 * RB) + r * RB + (((c % PER) ^ f) << 4));
 }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(TcCfg<D>::THREADS, TcCfg<D>::CTAS)
+template <int D, bool BF16, int FMT>
+__global__ void __launch_bounds__(TcCfg<D, FMT != 0>::THREADS, TcCfg<D, FMT != 0>::CTAS)
 kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const int32_t* __restrict__ list, const int32_t* __restrict__ counts,
              float* __restrict__ part, float2* __restrict__ ml, int n_splits) {
-    using C = TcCfg<D>;
+    constexpr bool CODES = FMT != 0, I8 = FMT == SENTRY_I8;
+    using C = TcCfg<D, CODES>;
     constexpr int KN = C::KN;
+    constexpr bool OP_BF16 = BF16 && !CODES;          // operands of the products: codes are fp16 exactly, and Q and the weights meet them as fp16
     extern __shared__ uint8_t smem_raw[];
     __shared__ TcMisc misc_s;
     TcMisc* misc = &misc_s;
@@ -93,10 +107,14 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             ptx::mbar_init(ptx::smem_u32(&misc->p_full[t]), 4);
             ptx::mbar_init(ptx::smem_u32(&misc->o_full[t]), 1);
         }
+        if (CODES)
+            for (int m = 0; m < C::META; ++m) ptx::mbar_init(ptx::smem_u32(&misc->meta_full[m]), 1);
         misc->abort_flag = 0;
         ptx::fence_barrier_init();
-        ptx::prefetch_tensormap(&maps.k);
-        ptx::prefetch_tensormap(&maps.v);
+        if (!CODES) {
+            ptx::prefetch_tensormap(&maps.k);
+            ptx::prefetch_tensormap(&maps.v);
+        }
     }
     grid_dependency_wait();
     if (warp == 0) {
@@ -118,6 +136,41 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
     // Q of a row block, by all threads
     auto load_q = [&](int row0) {
         const int halves = rows - row0 > kTM ? 2 : 1;
+        if constexpr (CODES && BF16) {
+            // as fp16, a row to a warp, four on the way at once: scaled by a power of two so that the largest value lies in [1,2)
+            constexpr int W = (D + 63) / 64, STEP = C::THREADS / 32;
+            for (int r0 = warp; r0 < halves * kTM; r0 += 4 * STEP) {
+                uint32_t w[4][W];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + r0 + i * STEP;
+                    const bool in = row < rows && r0 + i * STEP < halves * kTM;
+                    const uint32_t* src = in ? (const uint32_t*)((const uint16_t*)a.Q + b * a.qs[0] + misc->head[row / a.Tq] * a.qs[1] + row % a.Tq * a.qs[2]) : nullptr;
+#pragma unroll
+                    for (int x = 0; x < W; ++x) w[i][x] = in && x * 32 + lane < D / 2 ? src[x * 32 + lane] : 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + i * STEP;
+                    if (r >= halves * kTM) break;
+                    uint32_t top = 0u;
+#pragma unroll
+                    for (int x = 0; x < W; ++x) top = max(top, max(w[i][x] & 0x7fffu, w[i][x] >> 16 & 0x7fffu));
+                    top = __reduce_max_sync(0xffffffffu, top);
+                    const int e = min(max((int)(top >> 7) - 127, -120), 120);       // (what is no number stays none)
+                    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+                    for (int x = 0; x < W; ++x) {
+                        const int at = x * 32 + lane;
+                        if (at < D / 2)
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(q_smem + (r >> 7) * C::TILE + tile_offset<C::RB>(r & 127, at >> 2) + (at & 3) * 4),
+                                         "r"(pack2<false>(__uint_as_float(w[i][x] << 16) * down, __uint_as_float(w[i][x] & 0xffff0000u) * down))
+                                         : "memory");
+                    }
+                    if (lane == 0) misc->c.q_scale[r] = __uint_as_float((uint32_t)(127 + e) << 23);
+                }
+            }
+        } else {
         for (int e = threadIdx.x; e < halves * kTM * (D / 8); e += C::THREADS) {
             const int r = e / (D / 8), c = e % (D / 8), row = row0 + r;
             const uint32_t dst = q_smem + (r >> 7) * C::TILE + tile_offset<C::RB>(r & 127, c);
@@ -129,6 +182,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             }
         }
         ptx::cp_async_commit();
+        }
     };
     load_q(blockIdx.y * 2 * kTM);                 // (on its way while the list is made)
     // present keys of the sample, in order: the first `count`, those of this CTA's list, or of one that was made before
@@ -139,12 +193,39 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
     const int32_t* far = list ? list + (size_t)b * a.Tk : nullptr;
     auto key_at = [&](int p) { return own ? (int)misc->list[p] : far ? far[p] : p; };
     const int tiles = (count + KN - 1) / KN, per_split = (tiles + n_splits - 1) / n_splits;
-    const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles), steps = t1 - t0;
+    const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles);
+    // A page's value scale goes into its keys' exponents, so that O needs no unit that follows the pages: in units of the largest one of this
+    // CTA's pages (vref), and 2^-100 of it at least.
+    float vref = 1.0f;
+    const int page_shift = CODES ? 31 - __clz(a.page) : 0;
+    if constexpr (CODES) {
+        uint32_t top = 0u;
+        const int32_t* pages = a.table + (size_t)b * a.max_pages;
+#pragma unroll 4
+        for (int p = (t0 * KN >> page_shift) + (int)threadIdx.x; p < a.max_pages && p << page_shift < min(t1 * KN, count); p += C::THREADS) {
+            const int id = pages[p];
+            if ((unsigned)id >= (unsigned)a.n_pages) continue;
+            const uint32_t v = __float_as_uint(a.v_scales[(size_t)id * a.Hk + g]) & 0x7fffffffu;
+            if (v < 0x7f800000u) top = max(top, v);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) misc->c.top[warp] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < C::THREADS / 32; ++w) top = max(top, misc->c.top[w]);
+        vref = top == 0u ? 1.0f : fmaxf(__uint_as_float(top), 7.5231638e-37f);     // (2^-120)
+    }
     uint32_t done = 0;                            // steps of the row blocks before
+    int steps = 0;
 
     for (int rb = blockIdx.y; rb * 2 * kTM < rows; rb += gridDim.y, done += (uint32_t)steps) {
         const int row0 = rb * 2 * kTM;
         const int halves = rows - row0 > kTM ? 2 : 1;
+        steps = t1 - t0;
+        if (CODES && a.causal) {                  // no row of these sees more
+            const int end = min(row0 + 2 * kTM, rows) - 1, i = end / a.Tq != row0 / a.Tq ? a.Tq - 1 : end % a.Tq, seen = max(count - a.Tq + i + 1, 0);
+            steps = max(min(t1, (seen + KN - 1) / KN) - t0, 0);
+        }
         if (rb != (int)blockIdx.y) load_q(row0);
         ptx::cp_async_wait_all();
         ptx::fence_proxy_async_smem();
@@ -154,6 +235,91 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             const int lw = warp - C::LOAD_WARP0;
             const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
             bool ok = true;
+            if constexpr (CODES) {
+                // 16 codes a lane at a time, as fp16; zeros for keys that are not there.  K's and V's codes of the next step are on their way to
+                // registers while this one's are converted, and its pages' numbers a step before those.
+                constexpr int PER = D / 16, ROWS = C::LOAD_WARPS * 32 / PER, IT = (KN + ROWS - 1) / ROWS;
+                const int first = (lw * 32 + lane) / PER, c = (lw * 32 + lane) % PER;          // this lane's rows: first + i ROWS
+                const int32_t* pages = a.table + (size_t)b * a.max_pages;
+                const float inv_vref = 1.0f / vref;
+                auto page_of = [&](int j) {                 // of 16 keys of a step, a lane each
+                    const int p = (t0 + j) * KN + lane * 16;
+                    const int id = j < steps && lane < KN / 16 && p < count ? pages[p >> page_shift] : -1;
+                    if (id != -1 && (unsigned)id >= (unsigned)a.n_pages) return -2;      // (an entry that is needed, and no page; -1 counts below)
+                    return id;
+                };
+                struct Step { int id; float ks, vs; };
+                auto of_page = [&](int id) {
+                    Step x = {id, 0.0f, 0.0f};
+                    if (id >= 0) { x.ks = a.k_scales[(size_t)id * a.Hk + g]; x.vs = a.v_scales[(size_t)id * a.Hk + g]; }
+                    return x;
+                };
+                auto fetch = [&](uint4 (&v)[IT], const uint8_t* codes, int j, int id) {
+                    const int p0 = (t0 + j) * KN;
+#pragma unroll
+                    for (int i = 0; i < IT; ++i) {
+                        const int r = first + i * ROWS;
+                        const int at = __shfl_sync(0xffffffffu, id, (r >> 4) & 31);
+                        const bool here = r < KN && at >= 0 && p0 + r < count;
+                        v[i] = here ? *reinterpret_cast<const uint4*>(codes + (((size_t)at * a.Hk + g) * a.page + ((p0 + r) & (a.page - 1))) * D + c * 16) : make_uint4(0, 0, 0, 0);
+                    }
+                };
+                // sign: of the values of 16 keys, a lane each; -1: all are zero
+                auto convert = [&](const uint4 (&v)[IT], uint32_t dst, int sign) {
+#pragma unroll
+                    for (int i = 0; i < IT; ++i) {
+                        const int r = first + i * ROWS;
+                        const int how = __shfl_sync(0xffffffffu, sign, (r >> 4) & 31);
+                        if (r >= KN) continue;
+                        const uint32_t flip = how > 0 ? 0x80008000u : 0u, keep = how < 0 ? 0u : 0xffffffffu, w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        uint32_t f[8];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            codes_to_f16<I8>(w[x], f[2 * x], f[2 * x + 1]);
+                            f[2 * x] = (f[2 * x] ^ flip) & keep;
+                            f[2 * x + 1] = (f[2 * x + 1] ^ flip) & keep;
+                        }
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + tile_offset<C::RB>(r, 2 * c + x)), "r"(f[4 * x]), "r"(f[4 * x + 1]), "r"(f[4 * x + 2]),
+                                         "r"(f[4 * x + 3])
+                                         : "memory");
+                    }
+                    ptx::fence_proxy_async_smem();
+                };
+                uint4 kv[IT], vv[IT];
+                Step now = of_page(page_of(0));
+                int next = page_of(1);
+                fetch(kv, (const uint8_t*)a.K, 0, now.id);
+                fetch(vv, (const uint8_t*)a.V, 0, now.id);
+                for (int j = 0; j < steps && ok; ++j) {
+                    const uint32_t n = done + j, s = n % C::STAGES, use = n / C::STAGES, slot = n % C::META;
+                    const int p = (t0 + j) * KN + lane * 16;
+                    if (lw == 0 && lane < KN / 16 && p < count && now.id < 0) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+                    const unsigned holes = __ballot_sync(0xffffffffu, now.id < 0);
+                    const Step then = of_page(next);
+                    next = page_of(j + 2);
+                    ok = warp_wait(&misc->k_empty[s], (use & 1) ^ 1, abort_flag);
+                    if (!ok) break;
+                    if (lw == 0) {
+                        if (lane < KN / 16) {
+                            const float ratio = fabsf(now.vs) <= 3.4028234e38f ? fmaxf(fabsf(now.vs) * inv_vref, 7.8886091e-31f) : __int_as_float(0x7fc00000);    // (2^-100)
+                            misc->c.meta[slot][lane] = make_float4(now.ks, log2f(ratio), 1.0f / ratio, 0.0f);
+                        }
+                        if (lane == 0) misc->c.holes[slot] = holes;
+                        warp_arrive(&misc->meta_full[slot]);
+                    }
+                    convert(kv, k_smem + s * C::KTILE, 0);
+                    warp_arrive(&misc->k_full[s]);
+                    fetch(kv, (const uint8_t*)a.K, j + 1, then.id);
+                    ok = warp_wait(&misc->v_empty[s], (use & 1) ^ 1, abort_flag);
+                    if (!ok) break;
+                    convert(vv, v_smem + s * C::KTILE, now.vs == 0.0f ? -1 : now.vs < 0.0f);
+                    warp_arrive(&misc->v_full[s]);
+                    fetch(vv, (const uint8_t*)a.V, j + 1, then.id);
+                    now = then;
+                }
+            } else {
             // A tile that is gathered counts as here STAGES tiles (of K and V in turn) later, so that as many are on their way; what
             // the tiles' users wait for meanwhile lies before those.
             uint32_t gathered = 0;
@@ -209,10 +375,11 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             if (ok)
                 for (int back = C::STAGES - 1; back >= 0; --back)
                     if (gathered >> back & 1u) arrive(2 * steps - 1 - back);
+            }
         } else if (warp == C::ISSUE_WARP) {
             // ---------------------------------------------------------------- UMMAs
-            constexpr uint32_t qk = BF16 ? ptx::umma_idesc_bf16(kTM, KN) : ptx::umma_idesc_f16(kTM, KN);
-            constexpr uint32_t pv = BF16 ? ptx::umma_idesc_bf16_major(kTM, D, false, true) : ptx::umma_idesc_f16_major(kTM, D, false, true);
+            constexpr uint32_t qk = OP_BF16 ? ptx::umma_idesc_bf16(kTM, KN) : ptx::umma_idesc_f16(kTM, KN);
+            constexpr uint32_t pv = OP_BF16 ? ptx::umma_idesc_bf16_major(kTM, D, false, true) : ptx::umma_idesc_f16_major(kTM, D, false, true);
             bool ok = true;
             auto scores = [&](int t, uint32_t s) {
 #pragma unroll
@@ -267,8 +434,16 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
             const uint32_t sc = tmem + t * KN + lanes, oc = tmem + C::O_COL + t * D + lanes;
             const float c = rsqrtf((float)D) * kTcLog2e;
+            // what a score is multiplied by on its way to log2; those of a cache have been, with their page's scale and Q's
+            const float cm = CODES ? 1.0f : c;
+            float cq = c;
+            int last = count;                                  // keys that this row sees end here
+            if constexpr (CODES) {
+                if (BF16) cq *= misc->c.q_scale[t * kTM + (warp & 3) * 32 + lane];
+                if (a.causal) last = min(count, count - a.Tq + row % a.Tq + 1);
+            }
             // fp16 weights are taken 2^7 times as large (2^15 at most): its range is what small ones run out of
-            constexpr float kShift = BF16 ? 0.0f : 7.0f;
+            constexpr float kShift = OP_BF16 ? 0.0f : 7.0f;
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
             for (int j = 0; j < steps && ok && t < halves; ++j) {
@@ -276,35 +451,72 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 ok = warp_wait(&misc->s_full[t], n & 1, abort_flag);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                const int valid = count - (t0 + j) * KN;
+                const int valid = last - (t0 + j) * KN;
+                const uint32_t slot = n % C::META;
+                unsigned holes = 0u;
+                if constexpr (CODES) {
+                    ok = warp_wait(&misc->meta_full[slot], n / C::META & 1, abort_flag);
+                    if (!ok) break;
+                    holes = misc->c.holes[slot];
+                }
                 uint32_t s[KN / 32][32];
-                auto hide = [&](int z) {
+                auto settle = [&](int z) {
+                    if constexpr (CODES) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float4 page = misc->c.meta[slot][z * 2 + x];
+                            const uint64_t f = pair_f32(cq * page.x, cq * page.x), e = pair_f32(page.y, page.y);
+#pragma unroll
+                            for (int y = x * 16; y < x * 16 + 16; y += 2) {
+                                const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[z][y]), __uint_as_float(s[z][y + 1])), f, e));
+                                s[z][y] = __float_as_uint(u.x);
+                                s[z][y + 1] = __float_as_uint(u.y);
+                            }
+                        }
+                        if (holes >> (z * 2) & 3u) {
+#pragma unroll
+                            for (int y = 0; y < 32; ++y)
+                                if (holes >> (z * 2 + (y >> 4)) & 1u) s[z][y] = 0xff800000u;
+                        }
+                    }
                     if (valid < KN) {
 #pragma unroll
                         for (int y = 0; y < 32; ++y)
                             if (z * 32 + y >= valid) s[z][y] = 0xff800000u;
                     }
                 };
-#pragma unroll
-                for (int z = 0; z < KN / 32; ++z) ptx::tmem_ld_32x32(sc + z * 32, s[z]);
-                ptx::tmem_ld_wait();
-#pragma unroll
-                for (int z = 0; z < KN / 32; ++z) hide(z);
                 // (a score that is not a number makes the maximum one, and with it the whole row)
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto look = [&](int z) {
+                    settle(z);
 #pragma unroll
-                for (int y = 0; y < KN; y += 2) top[(y >> 1) & 3] = max3_nan(top[(y >> 1) & 3], __uint_as_float(s[y / 32][y % 32]), __uint_as_float(s[y / 32][y % 32 + 1]));
+                    for (int y = 0; y < 32; y += 2) top[(y >> 1) & 3] = max3_nan(top[(y >> 1) & 3], __uint_as_float(s[z][y]), __uint_as_float(s[z][y + 1]));
+                };
+                if constexpr (CODES) {              // (one block of scores in registers at a time)
+#pragma unroll
+                    for (int z = 0; z < KN / 32; ++z) {
+                        ptx::tmem_ld_32x32(sc + z * 32, s[z]);
+                        ptx::tmem_ld_wait();
+                        look(z);
+                    }
+                } else {
+#pragma unroll
+                    for (int z = 0; z < KN / 32; ++z) ptx::tmem_ld_32x32(sc + z * 32, s[z]);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int z = 0; z < KN / 32; ++z) look(z);
+                }
                 const float now = max3_nan(max3_nan(m, top[0], top[1]), top[2], top[3]);
                 if (j == 0) m = now;
                 else {
-                    const bool grew = !((now - m) * c <= 8.0f);
+                    const bool grew = !((now - m) * cm <= 8.0f);
                     if (__any_sync(0xffffffffu, grew)) {
                         // O follows the maximum; the last product into it has to be complete
                         ok = warp_wait(&misc->o_full[t], (n - 1) & 1, abort_flag);
                         if (!ok) break;
                         ptx::tc_fence_after_sync();
                         // (each row for itself: what its neighbours hold changes no bit of it)
-                        const float keep = grew && m != now ? exp2_fast((m - now) * c) : 1.0f;
+                        const float keep = grew && m != now ? exp2_fast((m - now) * cm) : 1.0f;
                         if (grew) m = now;
                         l *= keep;
 #pragma unroll
@@ -318,8 +530,8 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                         }
                     }
                 }
-                const float mc = (m == -INFINITY ? 0.0f : m * c) - kShift;
-                const uint64_t cc = pair_f32(c, c), mcc = pair_f32(-mc, -mc), one = pair_f32(1.0f, 1.0f);
+                const float mc = (m == -INFINITY ? 0.0f : m * cm) - kShift;
+                const uint64_t cc = pair_f32(cm, cm), mcc = pair_f32(-mc, -mc), one = pair_f32(1.0f, 1.0f);
                 uint64_t sum[2] = {pair_f32(0.0f, 0.0f), pair_f32(0.0f, 0.0f)};
 #pragma unroll
                 for (int z = 0; z < KN / 32; ++z) {
@@ -327,19 +539,30 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     if (z >= C::HELD) {                // (read again: the registers do not hold them all)
                         ptx::tmem_ld_32x32(sc + z * 32, s[z]);
                         ptx::tmem_ld_wait();
-                        hide(z);
+                        settle(z);
                     }
 #pragma unroll
                     for (int y = 0; y < 16; ++y) {
+                        if constexpr (CODES) {         // a weight counts in the sum without its page's value scale
+                            if (y % 8 == 0) sum[0] = sum[1] = pair_f32(0.0f, 0.0f);
+                        }
                         const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[z][2 * y]), __uint_as_float(s[z][2 * y + 1])), cc, mcc));
                         const float p0 = exp2_fast(u.x), p1 = exp2_fast(u.y);
                         sum[y & 1] = fma_pair(pair_f32(p0, p1), one, sum[y & 1]);
-                        w[y] = pack2<BF16>(p0, p1);
+                        w[y] = pack2<OP_BF16>(p0, p1);
+                        if constexpr (CODES) {
+                            if (y % 8 == 7) {
+                                const float2 x0 = pair_of(sum[0]), x1 = pair_of(sum[1]);
+                                const float group = (x0.x + x0.y) + (x1.x + x1.y);
+                                // (keys that this row does not see add nothing, whatever their page's scale is)
+                                l += group != 0.0f ? group * misc->c.meta[slot][z * 2 + (y >> 3)].z : 0.0f;
+                            }
+                        }
                     }
                     ptx::tmem_st_32x16(sc + z * 16, w);
                 }
                 const float2 sums[2] = {pair_of(sum[0]), pair_of(sum[1])};
-                l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+                if (!CODES) l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before_sync();
                 warp_arrive(&misc->p_full[t]);
@@ -351,8 +574,8 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 const bool in = row < rows;
                 const size_t each = (size_t)a.k_h * a.Tq, within = in ? (size_t)misc->pos[row / a.Tq] * a.Tq + row % a.Tq : 0;
                 const size_t out = b * each + within, pat = ((size_t)b * n_splits + split) * each + within;
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * c - kShift, l) : make_float2(-INFINITY, 0.0f);
+                const float inv = l == 0.0f ? 0.0f : vref / l;
+                if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * cm - kShift, l) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
                 for (int z = 0; z < D; z += 16) {
                     uint32_t o[16];
@@ -373,6 +596,8 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                         dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
                     } else if (steps > 0) {
                         uint4* dst = reinterpret_cast<uint4*>(part + pat * D + z);
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * vref);
 #pragma unroll
                         for (int y = 0; y < 4; ++y) dst[y] = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
                     }
@@ -430,8 +655,8 @@ long long row_blocks(const KvAttendArgs& a) {
     const long long n = ((long long)group_rows(a) + 2 * kTM - 1) / (2 * kTM);
     return n > 65535 ? 65535 : n;
 }
-int tc_keys(int d) { return d <= 64 ? TcCfg<64>::KN : TcCfg<128>::KN; }
-int tc_ctas(int d) { return d <= 64 ? TcCfg<64>::CTAS : TcCfg<128>::CTAS; }
+int tc_keys(int d) { return d <= 64 ? TcCfg<64, false>::KN : TcCfg<128, false>::KN; }
+int tc_ctas(int d) { return d <= 64 ? TcCfg<64, false>::CTAS : TcCfg<128, false>::CTAS; }
 // Blocks along the keys: where the row blocks alone leave SMs idle, each with two steps at least.
 int tc_splits(const KvAttendArgs& a) {
     const long long units = (long long)a.B * a.Hk * row_blocks(a);
@@ -443,11 +668,11 @@ int tc_splits(const KvAttendArgs& a) {
 }
 bool tc_planned(const KvAttendArgs& a) { return a.ids != nullptr && a.Tk > kTcListed; }
 
-template <int D, bool BF16>
+template <int D, bool BF16, int FMT>
 int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
-    using C = TcCfg<D>;
-    KvMaps maps;
-    if (!make_map_dense(&maps.k, a.K, a, a.ks, C::KN) || !make_map_dense(&maps.v, a.V, a, a.vs, C::KN)) return SENTRY_ERR_CUDA;
+    using C = TcCfg<D, FMT != 0>;
+    KvMaps maps = {};
+    if (FMT == 0 && (!make_map_dense(&maps.k, a.K, a, a.ks, C::KN) || !make_map_dense(&maps.v, a.V, a, a.vs, C::KN))) return SENTRY_ERR_CUDA;
     const int n_splits = tc_splits(a);
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     float* part = nullptr;
@@ -466,7 +691,7 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
         LaunchScope ls(ctx, KS_KV_PLAN, st);
         SENTRY_CUDA_TRY(launch_chained(kv_plan_kernel, dim3((unsigned)a.B), dim3(1024), 0, st, a, list, counts));
     }
-    auto k = kv_tc_kernel<D, BF16>;
+    auto k = kv_tc_kernel<D, BF16, FMT>;
     static std::atomic<unsigned long long> allowed{0};
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
     {
@@ -477,20 +702,24 @@ int launch_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t 
     return n_splits > 1 ? launch_kv_combine(ctx, a, part, ml, n_splits, st) : SENTRY_OK;
 }
 
-template <bool BF16>
+template <bool BF16, int FMT>
 int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
     switch (a.d) {
-        case 16: return launch_tc<16, BF16>(ctx, a, ws, st);
-        case 32: return launch_tc<32, BF16>(ctx, a, ws, st);
-        case 64: return launch_tc<64, BF16>(ctx, a, ws, st);
-        default: return launch_tc<128, BF16>(ctx, a, ws, st);
+        case 16: return launch_tc<16, BF16, FMT>(ctx, a, ws, st);
+        case 32: return launch_tc<32, BF16, FMT>(ctx, a, ws, st);
+        case 64: return launch_tc<64, BF16, FMT>(ctx, a, ws, st);
+        default: return launch_tc<128, BF16, FMT>(ctx, a, ws, st);
     }
 }
 
 }  // namespace
 
+// Dense keys: beyond the few rows that kv_rows_kernel packs into two tiles (33 rows cost either the same).  A cache: beyond 64 rows, where decoding the
+// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 160 us against 619;
+// 384 of 64 groups on 1024, d 64: 51 against 92; 128 of 64 groups on 2048, d 128: 50 against 92, 64 of them 46 against 49; 48 of 16 groups on
+// 8192, d 64: 36 against 31).
 bool kv_tc_takes(const KvAttendArgs& a) {
-    return a.format == 0 && a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > 32;
+    return a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > (a.format == 0 ? 32 : 64);
 }
 size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     const int n = tc_splits(a);
@@ -502,5 +731,8 @@ size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     return bytes + align_up((size_t)a.B * a.Tk * sizeof(int32_t), 256) + align_up((size_t)a.B * sizeof(int32_t), 256) + 512;
 }
 int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
-    return a.dtype == SENTRY_BF16 ? launch_tc_d<true>(ctx, a, ws, st) : launch_tc_d<false>(ctx, a, ws, st);
+    const bool bf16 = a.dtype == SENTRY_BF16;
+    if (a.format == 0) return bf16 ? launch_tc_d<true, 0>(ctx, a, ws, st) : launch_tc_d<false, 0>(ctx, a, ws, st);
+    if (a.format == SENTRY_FP8_E4M3) return bf16 ? launch_tc_d<true, SENTRY_FP8_E4M3>(ctx, a, ws, st) : launch_tc_d<false, SENTRY_FP8_E4M3>(ctx, a, ws, st);
+    return bf16 ? launch_tc_d<true, SENTRY_I8>(ctx, a, ws, st) : launch_tc_d<false, SENTRY_I8>(ctx, a, ws, st);
 }

@@ -691,3 +691,68 @@ def test_sizes_of_one(sn):
     odd = torch.randn(8 * 32 + 7, generator=g, device="cuda").bfloat16()
     q = torch.as_strided(odd, (1, 8, 1, 32), (3, 32, 5, 1))          # (no index ever multiplies the 3 and the 5)
     assert torch.equal(sn.cross_attend_fwd(q, K[:1], V[:1]), sn.cross_attend_fwd(q.clone(memory_format=torch.contiguous_format), K[:1], V[:1]))
+
+
+# (prompts of many rows on a cache: fmt, dtype, B, Tq, cols, page, Hq, Hk, d, k_h, causal)
+PROMPTS = [("i8", "bf16", 3, 40, 6, 16, 8, 2, 128, 8, 1), ("e4m3", "f16", 2, 200, 4, 128, 4, 2, 128, 3, 0), ("e4m3", "bf16", 5, 70, 9, 64, 2, 1, 128, 2, 1),
+           ("i8", "f16", 1, 1000, 10, 128, 2, 2, 64, 2, 1), ("e4m3", "f16", 2, 129, 70, 16, 2, 2, 32, 2, 0), ("i8", "bf16", 9, 65, 3, 32, 4, 4, 16, 4, 1),
+           ("i8", "f16", 1, 65, 90, 64, 1, 1, 128, 1, 0), ("e4m3", "bf16", 2, 700, 30, 16, 4, 4, 64, 2, 1)]
+
+
+@pytest.mark.parametrize("case", PROMPTS, ids=lambda c: "-".join(map(str, c)))
+def test_cache_attend_prompts(sn, case):
+    test_cache_attend(sn, case)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("Tq,N,d,page", [(200, 900, 64, 64), (300, 2000, 128, 16), (140, 333, 32, 128)])
+def test_rising_scores_cache_prompts(sn, fmt, dtype, Tq, N, d, page):
+    test_rising_scores_cache(sn, fmt, dtype, Tq, N, d, page)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("Tq", [1, 9, 150])
+def test_scales_of_any_sign(sn, fmt, dtype, Tq):
+    """Pages whose scales are somebody else's: negative, zero, a thousand times the others'."""
+    rng = np.random.default_rng(21)
+    B, Hq, Hk, d, page, cols = 2, 2, 1, 64, 16, 12
+    (kc, ks), (vc, vs) = (_pool(rng, B * cols, Hk, page, d, fmt) for _ in range(2))
+    kc = (kc // 8).astype(np.int8) if fmt == "i8" else np.where(kc & 127 > 0x58, kc & 0xd8, kc).astype(np.uint8)
+    ks[3::5] *= -1
+    ks[4::7] = 0
+    vs[1::3] *= -1
+    vs[2::5] = 0
+    vs[6::7] *= 1000
+    table = np.arange(B * cols, dtype=np.int32).reshape(B, cols)
+    lengths = np.array([cols * page, 101], np.int32)
+    Q = torch.randn((B, Hq, Tq, d), generator=torch.Generator().manual_seed(3)).to(DT[dtype])
+    O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, lengths), causal=True)
+    k, v = (ref.values(c, fmt) * s[..., None, None].astype(np.float64) for c, s in ((kc, ks), (vc, vs)))
+
+    def keys_of(b, g):
+        n = int(lengths[b])
+        kk, vv = (x[table[b]][:, g].reshape(-1, d)[:n] for x in (k, v))
+        return kk, vv, np.arange(n)[None] <= np.arange(Tq)[:, None] + n - Tq
+    _check_attention(O, Q, None, 2, keys_of, DT[dtype], 2.0 ** -11 if dtype != "f32" else 0.0, q16=dtype == "bf16")
+    assert sn.last_status() == 0
+
+
+def test_prompts_on_two_streams(sn):
+    """Blocks of many rows on a cache whose axis is split, from two contexts at once, in turn with single tokens."""
+    calls = [_cache_call(*s, seed=30 + i) for i, s in enumerate([(2, 90, 60, 32, 4, 2, 128), (3, 1, 300, 16, 8, 1, 128), (1, 300, 40, 64, 4, 1, 64)])]
+    alone = [sn.cache_attend_fwd(*c) for c in calls]
+    torch.cuda.synchronize()
+    other = sentry.Sentry(0)
+    try:
+        streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+        for i in range(24):
+            for s, st in zip((sn, other), streams):
+                with torch.cuda.stream(st):
+                    got.append((i % 3, s.cache_attend_fwd(*calls[i % 3])))
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, alone[i]) for i, o in got)
+        assert sn.last_status() == 0 and other.last_status() == 0
+    finally:
+        other.close()
