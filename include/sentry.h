@@ -585,8 +585,8 @@ SENTRY_API int sentry_cache_append(sentry_ctx* ctx, const sentry_kv_cache* cache
  * A row without a visible key is zero.  Lengths outside [0, max_pages * page] are clamped.
  * 16-bit Q meets the codes as fp16, each row scaled by a power of two so that its largest value lies in [1,2) (what the row has
  * below 2^-14 of it loses digits); the softmax weights are fp16 too, in the form for few rows as a head and a remainder where O
- * is fp16; all sums are fp32.  Value scales of one sample's pages may differ by 2^64; one that is smaller yet counts as larger
- * than it is.
+ * is fp16; all sums are fp32.  Value scales of the pages that a sample sees may differ by 2^64; values of pages smaller
+ * yet lose digits.
  * e4m3 codes 0x7f and 0xff (NaN; sentry_cache_append writes none) give NaN.  Workspace: sentry_cache_workspace_bytes.
  */
 typedef struct sentry_cache_attend_desc {
