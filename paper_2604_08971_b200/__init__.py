@@ -273,6 +273,9 @@ class Sentry:
             if self._captured:
                 self._kept_ws.append(self._ws)
                 self._captured = torch.cuda.is_current_stream_capturing()
+            elif self._ws is not None:
+                # (the calls before this one may still run on a stream that it was not allocated on)
+                self._ws.record_stream(torch.cuda.current_stream(self.device))
             self._ws = torch.empty((int(nbytes),), dtype=torch.uint8, device="cuda:%d" % self.device)
             rc = self.lib.sentry_set_workspace(self.h, self._ws.data_ptr(), self._ws.numel())
             if rc != 0:

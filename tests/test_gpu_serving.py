@@ -756,3 +756,32 @@ def test_prompts_on_two_streams(sn):
         assert sn.last_status() == 0 and other.last_status() == 0
     finally:
         other.close()
+
+
+def test_workspace_outgrown_on_another_stream():
+    """A workspace from one stream's memory, used on another stream and replaced there while the call that uses it still waits: whoever
+    allocates on the first stream does not get it until then."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    Q, K, V = (torch.randn((2, h, t, 64), generator=g, device="cuda").bfloat16() for h, t in ((4, 1), (1, 6000), (1, 6000)))
+    big = [torch.randn((8, h, t, 128), generator=g, device="cuda").bfloat16() for h, t in ((32, 8), (4, 6000), (4, 6000))]
+    s = sentry.Sentry(0)
+    try:
+        want = s.cross_attend_fwd(Q, K, V)
+        size, side = s._ws.numel(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        a = torch.randn((4096, 4096), device="cuda")
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                a = a @ a * 1e-3                          # keeps the stream busy for some ten milliseconds
+            O = s.cross_attend_fwd(Q, K, V)
+            s.cross_attend_fwd(*big)
+        assert s._ws.numel() > size
+        junk = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        for _ in range(200):
+            for j in junk:
+                j.fill_(255)
+        torch.cuda.synchronize()
+        assert torch.equal(O, want)
+    finally:
+        s.close()
