@@ -17,7 +17,7 @@ BINDING_STAMP = BINDING + ".stamp"   # what the binding was compiled against
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC",
-         "-shared", "-Xcompiler", "-fvisibility=hidden", "-Xcompiler", "-Wall"]
+         "-shared", "-Xcompiler", "-fvisibility=hidden", "-Xcompiler", "-Wall", "--threads", "0"]
 
 
 def sources():
