@@ -84,6 +84,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 struct RowsShare { int b, split, n, first, len; };   // first: number of the sample's first part among all samples' parts; len: its keys
 __device__ __forceinline__ RowsShare rows_share(const KvAttendArgs& a, int unit, int room) {
     const int lane = threadIdx.x & 31;
+    if (a.lengths == nullptr) {             // all alike: no search
+        const int each = min((room + a.B) / a.B, max(1, (a.Tk + kKeys - 1) / kKeys / kWarps)), b = unit / each;
+        return RowsShare{b < a.B ? b : -1, unit % each, each, b * each, a.Tk};
+    }
     auto length_of = [&](int b) { return b < a.B ? kv_length(a, b) : 0; };
     auto tiles = [](int len) { return (len + kKeys - 1) / kKeys; };
     const int mine = length_of(lane);
@@ -215,6 +219,22 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
     const int len = share.len;
     const int tiles = (len + kKeys - 1) / kKeys;
     const int t0 = (int)((long long)tiles * share.split / share.n), t1 = (int)((long long)tiles * (share.split + 1) / share.n);
+    // the copying warp: of 32 tiles at a time, a lane each, the pages of the first 16 keys and of the others (-1: none)
+    const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
+    int id0 = -1, id1 = -1;
+    auto ask_pages = [&](int tile) {
+        const int32_t* pages = a.table + (size_t)b * a.max_pages;
+        const int n = (tile + lane) * kKeys;
+        const bool in = tile + lane < t1, second = in && n + 16 < len;
+        id0 = in ? pages[n >> page_shift] : -1;
+        id1 = page_shift > 4 ? id0 : second ? pages[(n >> 4) + 1] : -1;
+        const bool bad0 = in && (unsigned)id0 >= (unsigned)a.n_pages, bad1 = second && (unsigned)id1 >= (unsigned)a.n_pages;
+        if (bad0 || bad1) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
+        if ((unsigned)id0 >= (unsigned)a.n_pages) id0 = -1;
+        if ((unsigned)id1 >= (unsigned)a.n_pages) id1 = -1;
+    };
+    if constexpr (!DENSE)
+        if (warp == kWarps) ask_pages(t0);                  // (while another warp reads the list of heads)
     __syncthreads();
     const int rows = s_heads * a.Tq;
     uint32_t done = 0;                                      // tiles of the row tiles before
@@ -225,10 +245,6 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
             // ---------------------------------------------------------------- copies
             const uint32_t mask = a.masks ? a.masks[b] : 0u;
             const int kb = a.ks[0] ? b : 0, kg = a.ks[1] ? g : 0, vb = a.vs[0] ? b : 0, vg = a.vs[1] ? g : 0;
-            const int32_t* pages = DENSE ? nullptr : a.table + (size_t)b * a.max_pages;
-            const int page_shift = DENSE ? 0 : 31 - __clz(a.page);
-            // of 32 tiles at a time, a lane each: the pages of the first 16 keys and of the others (-1: none)
-            int id0 = -1, id1 = -1;
             int ahead = DENSE && a.ids != nullptr && t0 * kKeys + lane < len ? a.ids[t0 * kKeys + lane] : 0;
             uint32_t s = done % C::STAGES, use = done / C::STAGES;
             for (int tile = t0; tile < t1 && ok; ++tile) {
@@ -244,15 +260,7 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
                     vis = __ballot_sync(0xffffffffu, here);
                 } else {
                     const int turn = (tile - t0) & 31;
-                    if (turn == 0) {
-                        const int n = (tile + lane) * kKeys;
-                        id0 = tile + lane < t1 ? pages[n >> page_shift] : -1;
-                        id1 = page_shift > 4 ? id0 : tile + lane < t1 && n + 16 < len ? pages[(n >> 4) + 1] : -1;
-                        const bool bad0 = tile + lane < t1 && (unsigned)id0 >= (unsigned)a.n_pages, bad1 = tile + lane < t1 && n + 16 < len && (unsigned)id1 >= (unsigned)a.n_pages;
-                        if (bad0 || bad1) atomicOr(a.status, SENTRY_STATUS_BIT_BAD_INDEX);
-                        if ((unsigned)id0 >= (unsigned)a.n_pages) id0 = -1;
-                        if ((unsigned)id1 >= (unsigned)a.n_pages) id1 = -1;
-                    }
+                    if (turn == 0 && (tile > t0 || (t1 - t0 > 32 && done > 0))) ask_pages(tile);
                     at0 = __shfl_sync(0xffffffffu, id0, turn);
                     at1 = __shfl_sync(0xffffffffu, id1, turn);
                     vis = len - n0 >= 32 ? 0xffffffffu : (1u << (len - n0)) - 1u;
