@@ -18,6 +18,8 @@
 // where they do not: the last tile of a sample, and tiles across the border of a missing modality.
 // A cache's codes are made fp16 by the loading warps, exactly; Q and the weights meet them as fp16.  A page's key scale multiplies its scores, and the
 // logarithm of its value scale is added to them, so that the weights carry it and O needs no unit of its own; the sum takes it out again.
+// (A step of two tiles of 128 rows on 128 codes, d 128: some 6000 cycles, against 3900 on dense keys: the loading warps' conversions and the softmax's, which at 16
+// warps has 128 registers a thread.  Three loading warps with 168 183 us, seven 160, five 159, and four whose rows lie a multiple of 16 apart 148.)
 // Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"
@@ -39,7 +41,7 @@ struct TcCfg {
     static constexpr int KN = D <= 64 ? 64 : 128;            // keys of a step
     static constexpr int CTAS = KN == 64 ? 2 : 1;            // of an SM
     // after the four softmax warps of each tile; then one issuer.  (Who makes 16 bits of codes has more to do than who waits for copies.)
-    static constexpr int LOAD_WARPS = CODES ? (KN == 64 ? 3 : 7) : KN == 64 ? 1 : 3;
+    static constexpr int LOAD_WARPS = CODES ? (KN == 64 ? 2 : 4) : KN == 64 ? 1 : 3;
     static constexpr int LOAD_WARP0 = 8, ISSUE_WARP = LOAD_WARP0 + LOAD_WARPS, THREADS = (ISSUE_WARP + 1) * 32;
     static constexpr int TMEM = 512 / CTAS, O_COL = 2 * KN;  // tensor memory: S of both tiles, then O of both
     static constexpr int RB = D >= 64 ? 128 : D * 2;         // bytes of a shared-memory row (64 elements at most)
@@ -47,7 +49,7 @@ struct TcCfg {
     static constexpr int SLAB = kTM * RB, TILE = SLABS * SLAB;         // of Q: 128 rows of D elements
     static constexpr int KSLAB = KN * RB, KTILE = SLABS * KSLAB;       // of K and V
     static constexpr int STAGES = D == 128 ? 2 : 4;          // of K, and of V
-    static constexpr int HELD = CODES ? 0 : KN == 64 ? 1 : 3;  // blocks of 32 scores that a thread keeps from the maximum to the weights
+    static constexpr int HELD = KN == 64 ? 1 : CODES ? 2 : 3;   // blocks of 32 scores that a thread keeps from the maximum to the weights
     static constexpr int META = 2 * STAGES;                  // steps whose pages' scales are kept: what a reader of one needs lies at most STAGES ahead
     static constexpr int SMEM = 2 * TILE + 2 * STAGES * KTILE + 1024;
     static_assert(O_COL + 2 * D <= TMEM && (KN == 128 || SLABS == 1), "tensor memory, and slabs of 128 rows");
@@ -238,8 +240,12 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
             if constexpr (CODES) {
                 // 16 codes a lane at a time, as fp16; zeros for keys that are not there.  K's and V's codes of the next step are on their way to
                 // registers while this one's are converted, and its pages' numbers a step before those.
+                // A lane's rows lie a multiple of 16 apart, so that their places in a page, in the tile and in its swizzle differ by constants.
                 constexpr int PER = D / 16, ROWS = C::LOAD_WARPS * 32 / PER, IT = (KN + ROWS - 1) / ROWS;
+                static_assert(ROWS % 16 == 0 && ROWS <= KN, "rows of a lane");
                 const int first = (lw * 32 + lane) / PER, c = (lw * 32 + lane) % PER;          // this lane's rows: first + i ROWS
+                const uint32_t to0 = tile_offset<C::RB>(first, 2 * c), to1 = tile_offset<C::RB>(first, 2 * c + 1);
+                const uint32_t lane_at = (first & 15) * D + c * 16;
                 const int32_t* pages = a.table + (size_t)b * a.max_pages;
                 const float inv_vref = 1.0f / vref;
                 auto page_of = [&](int j) {                 // of 16 keys of a step, a lane each
@@ -254,44 +260,48 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     if (id >= 0) { x.ks = a.k_scales[(size_t)id * a.Hk + g]; x.vs = a.v_scales[(size_t)id * a.Hk + g]; }
                     return x;
                 };
-                auto fetch = [&](uint4 (&v)[IT], const uint8_t* codes, int j, int id) {
+                auto fetch = [&](uint4 (&v)[IT], const void* codes, int j, int id) {
                     const int p0 = (t0 + j) * KN;
+                    // (rows of the pool: below 2^31)
+                    const int row = id < 0 ? -1 : (id * a.Hk + g) * a.page + ((p0 + lane * 16) & (a.page - 1));
 #pragma unroll
                     for (int i = 0; i < IT; ++i) {
-                        const int r = first + i * ROWS;
-                        const int at = __shfl_sync(0xffffffffu, id, (r >> 4) & 31);
-                        const bool here = r < KN && at >= 0 && p0 + r < count;
-                        v[i] = here ? *reinterpret_cast<const uint4*>(codes + (((size_t)at * a.Hk + g) * a.page + ((p0 + r) & (a.page - 1))) * D + c * 16) : make_uint4(0, 0, 0, 0);
+                        const int r = first + i * ROWS, at = __shfl_sync(0xffffffffu, row, r >> 4);
+                        v[i] = at >= 0 && p0 + r < count ? *reinterpret_cast<const uint4*>((const uint8_t*)codes + (size_t)at * D + lane_at) : make_uint4(0, 0, 0, 0);
                     }
                 };
                 // sign: of the values of 16 keys, a lane each; -1: all are zero
                 auto convert = [&](const uint4 (&v)[IT], uint32_t dst, int sign) {
+                    const bool signs = __any_sync(0xffffffffu, sign != 0);
 #pragma unroll
                     for (int i = 0; i < IT; ++i) {
-                        const int r = first + i * ROWS;
-                        const int how = __shfl_sync(0xffffffffu, sign, (r >> 4) & 31);
-                        if (r >= KN) continue;
-                        const uint32_t flip = how > 0 ? 0x80008000u : 0u, keep = how < 0 ? 0u : 0xffffffffu, w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                         uint32_t f[8];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            codes_to_f16<I8>(w[x], f[2 * x], f[2 * x + 1]);
-                            f[2 * x] = (f[2 * x] ^ flip) & keep;
-                            f[2 * x + 1] = (f[2 * x + 1] ^ flip) & keep;
-                        }
+                        for (int x = 0; x < 4; ++x) codes_to_f16<I8>(w[x], f[2 * x], f[2 * x + 1]);
+                        if (signs) {
+                            const int how = __shfl_sync(0xffffffffu, sign, (first + i * ROWS) >> 4);
 #pragma unroll
-                        for (int x = 0; x < 2; ++x)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + tile_offset<C::RB>(r, 2 * c + x)), "r"(f[4 * x]), "r"(f[4 * x + 1]), "r"(f[4 * x + 2]),
-                                         "r"(f[4 * x + 3])
+                            for (int x = 0; x < 8; ++x) f[x] = how < 0 ? 0u : f[x] ^ (how > 0 ? 0x80008000u : 0u);
+                        }
+                        const uint32_t at = dst + i * ROWS * C::RB;
+                        // (two lanes of eight write to the second slab: in the other order, which keeps their banks apart)
+                        const bool turned = C::SLABS == 2 && c >= PER / 2;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const bool hi = (x == 1) != turned;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (hi ? to1 : to0)), "r"(hi ? f[4] : f[0]), "r"(hi ? f[5] : f[1]), "r"(hi ? f[6] : f[2]),
+                                         "r"(hi ? f[7] : f[3])
                                          : "memory");
+                        }
                     }
                     ptx::fence_proxy_async_smem();
                 };
                 uint4 kv[IT], vv[IT];
                 Step now = of_page(page_of(0));
                 int next = page_of(1);
-                fetch(kv, (const uint8_t*)a.K, 0, now.id);
-                fetch(vv, (const uint8_t*)a.V, 0, now.id);
+                fetch(kv, a.K, 0, now.id);
+                fetch(vv, a.V, 0, now.id);
                 for (int j = 0; j < steps && ok; ++j) {
                     const uint32_t n = done + j, s = n % C::STAGES, use = n / C::STAGES, slot = n % C::META;
                     const int p = (t0 + j) * KN + lane * 16;
@@ -311,12 +321,12 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     }
                     convert(kv, k_smem + s * C::KTILE, 0);
                     warp_arrive(&misc->k_full[s]);
-                    fetch(kv, (const uint8_t*)a.K, j + 1, then.id);
+                    fetch(kv, a.K, j + 1, then.id);
                     ok = warp_wait(&misc->v_empty[s], (use & 1) ^ 1, abort_flag);
                     if (!ok) break;
-                    convert(vv, v_smem + s * C::KTILE, now.vs == 0.0f ? -1 : now.vs < 0.0f);
+                    convert(vv, v_smem + s * C::KTILE, now.id < 0 ? 0 : now.vs == 0.0f ? -1 : now.vs < 0.0f);
                     warp_arrive(&misc->v_full[s]);
-                    fetch(vv, (const uint8_t*)a.V, j + 1, then.id);
+                    fetch(vv, a.V, j + 1, then.id);
                     now = then;
                 }
             } else {
@@ -715,8 +725,8 @@ int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
 }  // namespace
 
 // Dense keys: beyond the few rows that kv_rows_kernel packs into two tiles (33 rows cost either the same).  A cache: beyond 64 rows, where decoding the
-// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 160 us against 619;
-// 384 of 64 groups on 1024, d 64: 51 against 92; 128 of 64 groups on 2048, d 128: 50 against 92, 64 of them 46 against 49; 48 of 16 groups on
+// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 148 us against 619;
+// 384 of 64 groups on 1024, d 64: 46 against 92; 128 of 64 groups on 2048, d 128: 50 against 92, 64 of them 46 against 49; 48 of 16 groups on
 // 8192, d 64: 36 against 31).
 bool kv_tc_takes(const KvAttendArgs& a) {
     return a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > (a.format == 0 ? 32 : 64);
