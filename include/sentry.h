@@ -516,7 +516,7 @@ SENTRY_API int sentry_linear_i8(sentry_ctx* ctx, const sentry_linear_desc* desc,
  * Strides in elements, multiples of 8 for the 16-bit types and of 4 for F32 (a token's d values are contiguous; Q, K and V
  * may be views of one projection's result), at most 2^38; all three 0 = contiguous.  A batch or head stride of 0 shares one
  * tensor; a token stride of 0 of K or V with Tk > 1 is UNSUPPORTED.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
- * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24.
+ * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24, k_h * Tq < 2^30.
  * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (by 2^-8 and 2^-11 of
  * themselves at most), in the form for few rows as a rounded head and a remainder.  A row whose scores are all minus infinity
  * (from an infinite q or k) is zero.

@@ -26,6 +26,7 @@ int strides_of(const int64_t given[3], int H, int T, int d, int dtype, long long
 int check_heads(int B, int Tq, int Hq, int Hk, int d, int k_h) {
     if (B < 0 || Tq < 0 || Hq < 1 || Hk < 1 || k_h < 1 || Hq % Hk != 0 || k_h > Hq) return SENTRY_ERR_BAD_SHAPE;
     if (!head_dim(d) || Hq > kServeMaxHeads || Tq >= kMaxRows || (long long)B * Hq >= kMaxRows) return SENTRY_ERR_UNSUPPORTED;
+    if ((long long)k_h * Tq >= 1LL << 30) return SENTRY_ERR_UNSUPPORTED;      // a sample's rows are counted in 32 bits, a block's ahead
     return SENTRY_OK;
 }
 

@@ -62,7 +62,7 @@ def test_cross_refusals(lib, ctx):
     assert f(_cross(dtype=sentry.SENTRY_I8)) == INVALID
     for kw in (dict(B=-1), dict(Tq=-1), dict(Tk=-1), dict(Hq=0), dict(Hk=0), dict(k_h=0), dict(Hq=5), dict(k_h=5)):
         assert f(_cross(**kw)) == SHAPE, kw
-    for kw in (dict(d=48), dict(Hq=512, Hk=2), dict(Tq=1 << 24), dict(Tk=1 << 24), dict(B=1 << 23)):
+    for kw in (dict(d=48), dict(Hq=512, Hk=2), dict(Tq=1 << 24), dict(Tk=1 << 24), dict(B=1 << 23), dict(B=1, Tq=(1 << 24) - 1, Hq=128, Hk=1, k_h=128)):
         assert f(_cross(**kw)) == UNSUPPORTED, kw
     assert f(_cross(q_stride=(96, 4, 32))) == UNSUPPORTED and f(_cross(k_stride=(-8, 8, 8))) == SHAPE
     assert f(_cross(k_stride=(8, 32, 0))) == UNSUPPORTED and f(_cross(v_stride=(8, 32, 0))) == UNSUPPORTED   # one key for all
