@@ -12,14 +12,15 @@
 // Bound by the exponentials (16 a clock and SM) up to d 64, by those and the products together at d 128.  Up to d 64 a step is of 64 keys and
 // an SM holds two CTAs, four tiles that wait for one another's latencies (4 x 4096 rows on 8192 keys, 16 heads on 4, d 64, bf16: 830 us, against
 // 910 with one CTA and 128 keys; 32 samples of 211 rows on 648 keys, 7 of 12 heads on 4: 28 us against 32); at d 128 tensor memory has room for
-// one, whose steps are of 128 keys (the same rows at d 128: 917 us in a burst, 1.2 PFLOP/s; 1050 under the power limit).  Registers hold all but the
-// last 32 scores of a step from the maximum to the weights: those are read twice (all of them at d 128: 945 us, with spills).
+// one, whose steps are of 128 keys (the same rows at d 128: 917 us in a burst, 1.2 PFLOP/s; 1050 under the power limit).  On dense keys registers hold all
+// but the last 32 scores of a step from the maximum to the weights: those are read twice (none of them at d 128: 945 us, with spills).
 // Dense K and V come by TMA where the present keys of a step follow one another, and row by row (16-byte asynchronous copies, zeros for what is not there)
 // where they do not: the last tile of a sample, and tiles across the border of a missing modality.
 // A cache's codes are made fp16 by the loading warps, exactly; Q and the weights meet them as fp16.  A page's key scale multiplies its scores, and the
 // logarithm of its value scale is added to them, so that the weights carry it and O needs no unit of its own; the sum takes it out again.
-// (A step of two tiles of 128 rows on 128 codes, d 128: some 6000 cycles, against 3900 on dense keys: the loading warps' conversions and the softmax's, which at 16
-// warps has 128 registers a thread.  Three loading warps with 168 183 us, seven 160, five 159, and four whose rows lie a multiple of 16 apart 148.)
+// (A step of two tiles of 128 rows on 128 codes, d 128: some 6000 cycles, against 3900 on dense keys: the loading warps' conversions and the softmax's, which at 13
+// warps has 128 registers a thread, keeps no scores and runs 32 of them at a time through one loop.  2048 rows of 8 groups on 8192 tokens: 142 us; with the loop
+// unrolled and 64 scores kept 148; before that, three loading warps and 168 registers 183, five 159, seven 160, four whose rows lie a multiple of 16 apart 148.)
 // Every wait is bounded; on expiry the CTA raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"
@@ -49,7 +50,7 @@ struct TcCfg {
     static constexpr int SLAB = kTM * RB, TILE = SLABS * SLAB;         // of Q: 128 rows of D elements
     static constexpr int KSLAB = KN * RB, KTILE = SLABS * KSLAB;       // of K and V
     static constexpr int STAGES = D == 128 ? 2 : 4;          // of K, and of V
-    static constexpr int HELD = KN == 64 ? 1 : CODES ? 2 : 3;   // blocks of 32 scores that a thread keeps from the maximum to the weights
+    static constexpr int HELD = CODES ? 0 : KN == 64 ? 1 : 3;   // blocks of 32 scores that a thread keeps from the maximum to the weights
     static constexpr int META = 2 * STAGES;                  // steps whose pages' scales are kept: what a reader of one needs lies at most STAGES ahead
     static constexpr int SMEM = 2 * TILE + 2 * STAGES * KTILE + 1024;
     static_assert(O_COL + 2 * D <= TMEM && (KN == 128 || SLABS == 1), "tensor memory, and slabs of 128 rows");
@@ -469,43 +470,45 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     if (!ok) break;
                     holes = misc->c.holes[slot];
                 }
-                uint32_t s[KN / 32][32];
-                auto settle = [&](int z) {
+                uint32_t s[CODES ? 1 : KN / 32][32];
+                auto settle = [&](int z, float add) {              // (add: to what a cache's scores become; dense ones stay as they are)
+                    const int at = CODES ? 0 : z;
                     if constexpr (CODES) {
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
                             const float4 page = misc->c.meta[slot][z * 2 + x];
-                            const uint64_t f = pair_f32(cq * page.x, cq * page.x), e = pair_f32(page.y, page.y);
+                            const uint64_t f = pair_f32(cq * page.x, cq * page.x), e = pair_f32(page.y + add, page.y + add);
 #pragma unroll
                             for (int y = x * 16; y < x * 16 + 16; y += 2) {
-                                const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[z][y]), __uint_as_float(s[z][y + 1])), f, e));
-                                s[z][y] = __float_as_uint(u.x);
-                                s[z][y + 1] = __float_as_uint(u.y);
+                                const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[at][y]), __uint_as_float(s[at][y + 1])), f, e));
+                                s[at][y] = __float_as_uint(u.x);
+                                s[at][y + 1] = __float_as_uint(u.y);
                             }
                         }
                         if (holes >> (z * 2) & 3u) {
 #pragma unroll
                             for (int y = 0; y < 32; ++y)
-                                if (holes >> (z * 2 + (y >> 4)) & 1u) s[z][y] = 0xff800000u;
+                                if (holes >> (z * 2 + (y >> 4)) & 1u) s[at][y] = 0xff800000u;
                         }
                     }
                     if (valid < KN) {
 #pragma unroll
                         for (int y = 0; y < 32; ++y)
-                            if (z * 32 + y >= valid) s[z][y] = 0xff800000u;
+                            if (z * 32 + y >= valid) s[at][y] = 0xff800000u;
                     }
                 };
                 // (a score that is not a number makes the maximum one, and with it the whole row)
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 auto look = [&](int z) {
-                    settle(z);
+                    const int at = CODES ? 0 : z;
+                    settle(z, 0.0f);
 #pragma unroll
-                    for (int y = 0; y < 32; y += 2) top[(y >> 1) & 3] = max3_nan(top[(y >> 1) & 3], __uint_as_float(s[z][y]), __uint_as_float(s[z][y + 1]));
+                    for (int y = 0; y < 32; y += 2) top[(y >> 1) & 3] = max3_nan(top[(y >> 1) & 3], __uint_as_float(s[at][y]), __uint_as_float(s[at][y + 1]));
                 };
                 if constexpr (CODES) {              // (one block of scores in registers at a time)
-#pragma unroll
+#pragma unroll 1
                     for (int z = 0; z < KN / 32; ++z) {
-                        ptx::tmem_ld_32x32(sc + z * 32, s[z]);
+                        ptx::tmem_ld_32x32(sc + z * 32, s[0]);
                         ptx::tmem_ld_wait();
                         look(z);
                     }
@@ -543,20 +546,23 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 const float mc = (m == -INFINITY ? 0.0f : m * cm) - kShift;
                 const uint64_t cc = pair_f32(cm, cm), mcc = pair_f32(-mc, -mc), one = pair_f32(1.0f, 1.0f);
                 uint64_t sum[2] = {pair_f32(0.0f, 0.0f), pair_f32(0.0f, 0.0f)};
-#pragma unroll
+#pragma unroll(CODES ? 1 : KN / 32)
                 for (int z = 0; z < KN / 32; ++z) {
+                    const int at = CODES ? 0 : z;
                     uint32_t w[16];
                     if (z >= C::HELD) {                // (read again: the registers do not hold them all)
-                        ptx::tmem_ld_32x32(sc + z * 32, s[z]);
+                        ptx::tmem_ld_32x32(sc + z * 32, s[at]);
                         ptx::tmem_ld_wait();
-                        settle(z);
+                        settle(z, -mc);
                     }
 #pragma unroll
                     for (int y = 0; y < 16; ++y) {
                         if constexpr (CODES) {         // a weight counts in the sum without its page's value scale
                             if (y % 8 == 0) sum[0] = sum[1] = pair_f32(0.0f, 0.0f);
                         }
-                        const float2 u = pair_of(fma_pair(pair_f32(__uint_as_float(s[z][2 * y]), __uint_as_float(s[z][2 * y + 1])), cc, mcc));
+                        uint64_t u2 = pair_f32(__uint_as_float(s[at][2 * y]), __uint_as_float(s[at][2 * y + 1]));
+                        if (!CODES) u2 = fma_pair(u2, cc, mcc);
+                        const float2 u = pair_of(u2);
                         const float p0 = exp2_fast(u.x), p1 = exp2_fast(u.y);
                         sum[y & 1] = fma_pair(pair_f32(p0, p1), one, sum[y & 1]);
                         w[y] = pack2<OP_BF16>(p0, p1);
@@ -725,8 +731,8 @@ int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
 }  // namespace
 
 // Dense keys: beyond the few rows that kv_rows_kernel packs into two tiles (33 rows cost either the same).  A cache: beyond 64 rows, where decoding the
-// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 148 us against 619;
-// 384 of 64 groups on 1024, d 64: 46 against 92; 128 of 64 groups on 2048, d 128: 50 against 92, 64 of them 46 against 49; 48 of 16 groups on
+// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 142 us against 619;
+// 384 of 64 groups on 1024, d 64: 47 against 92; 128 of 64 groups on 2048, d 128: 46 against 92, 64 of them 46 against 49; 48 of 16 groups on
 // 8192, d 64: 36 against 31).
 bool kv_tc_takes(const KvAttendArgs& a) {
     return a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > (a.format == 0 ? 32 : 64);

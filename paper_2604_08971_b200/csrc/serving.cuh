@@ -34,7 +34,7 @@ struct KvAttendArgs {
 };
 int launch_kv_generic(sentry_ctx* ctx, const KvAttendArgs& a, cudaStream_t st);            // fp32 rows
 size_t kv_rows_ws_bytes(const KvAttendArgs& a);
-bool kv_tc_takes(const KvAttendArgs& a);                                                   // 16-bit dense, many rows
+bool kv_tc_takes(const KvAttendArgs& a);                                                   // 16-bit rows, many of them
 size_t kv_tc_ws_bytes(const KvAttendArgs& a);
 int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st);
 int launch_kv_combine(sentry_ctx* ctx, const KvAttendArgs& a, const float* part, const float2* ml, int n_splits, cudaStream_t st);
