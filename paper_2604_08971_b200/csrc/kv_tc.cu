@@ -730,12 +730,19 @@ int launch_tc_d(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_
 
 }  // namespace
 
-// Dense keys: beyond the few rows that kv_rows_kernel packs into two tiles (33 rows cost either the same).  A cache: beyond 64 rows, where decoding the
-// codes once for 256 rows outweighs a step's latency for 128 rows at least (2048 rows of 8 groups on 8192 i8 tokens, d 128: 142 us against 619;
-// 384 of 64 groups on 1024, d 64: 47 against 92; 128 of 64 groups on 2048, d 128: 46 against 92, 64 of them 46 against 49; 48 of 16 groups on
-// 8192, d 64: 36 against 31).
+// Which of the two 16-bit forms: kv_rows_kernel's work is its row tiles of 16 times their keys, 128 at a time, in a wave or two of small blocks; a CTA here has a
+// setup of several microseconds and takes 256 rows at once.
+// Dense keys, bf16 (here against there): 2 x 40 rows of 4 groups on 77 keys, d 64 (24 units) 8.2 against 6.2 us; 64 x 4 rows of 16 groups on 256 (512) 13.3
+// against 9.5; 20 x 3 of 64 on 300 (768) 12.5 against 10.4; 17 x 4 of 64 on 512 (1280) 10.8 against 12.3; 512 x 4 of 2 on 512 (1024) 13.6 against 19.6.  At d 128
+// only the smallest lose: 40 x 4 of 2 on 256 (40) 11.5 against 15.7.
+// A cache, i8: 75 x 2 of 6 on 128 (60) 16.7 against 7.5; 128 x 4 of 8 on 512 (1024) 32.5 against 19.0; 17 x 4 of 64 on 512 (1280) 17.6 against 15.8; 16 x 4 of 64
+// on 2048 (4096) 46 against 49; 24 x 4 of 16 on 8192 (6144) 37 against 52; 512 x 4 of 8 on 8192 (65536) 142 against 619; but 128 x 4 of 32 on 128 (1024 tiles, more than
+// a wave) 19.2 against 24.2.
 bool kv_tc_takes(const KvAttendArgs& a) {
-    return a.dtype != SENTRY_F32 && a.Tk > 0 && group_rows(a) > (a.format == 0 ? 32 : 64);
+    if (a.dtype == SENTRY_F32 || a.Tk == 0 || group_rows(a) <= (a.format == 0 ? 32 : 64)) return false;
+    const long long row_tiles = (long long)a.B * a.Hk * ((group_rows(a) + 15) / 16), work = row_tiles * (((long long)a.Tk + 127) / 128);
+    if (a.format == 0) return a.d > 64 || work > 768;
+    return work > 2048 || row_tiles > 4 * kSmCount;
 }
 size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     const int n = tc_splits(a);

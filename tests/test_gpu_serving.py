@@ -785,3 +785,83 @@ def test_workspace_outgrown_on_another_stream():
         assert torch.equal(O, want)
     finally:
         s.close()
+
+
+# (calls large enough for the form of many rows: as above, and views, bad heads, bad pages, odd scales, two streams for it)
+MANY = [("i8", "bf16", 3, 140, 10, 128, 8, 2, 128, 8, 1), ("e4m3", "f16", 4, 200, 32, 64, 4, 2, 128, 3, 0), ("e4m3", "bf16", 25, 70, 20, 64, 2, 1, 64, 2, 1),
+        ("i8", "f16", 1, 1000, 40, 128, 2, 2, 64, 2, 1), ("e4m3", "f16", 2, 129, 560, 16, 2, 2, 32, 2, 0), ("i8", "bf16", 40, 65, 24, 32, 4, 4, 16, 4, 1),
+        ("i8", "f16", 1, 65, 1000, 64, 1, 1, 128, 1, 0), ("e4m3", "bf16", 4, 700, 30, 16, 4, 4, 64, 2, 1)]
+
+
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(map(str, c)))
+def test_cache_attend_many_rows(sn, case):
+    test_cache_attend(sn, case)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 16)])
+def test_rising_scores_cache_many_rows(sn, fmt, dtype, d, page):
+    test_rising_scores_cache(sn, fmt, dtype, 2100, 2100, d, page)
+
+
+def test_cache_edges_many_rows(sn):
+    test_cache_attend_edges(sn, "bf16", 1200)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scales_of_any_sign_many_rows(sn, fmt, dtype):
+    test_scales_of_any_sign(sn, fmt, dtype, 5000)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", [(9, 100, 900, 4, 2, 16, 4, "both"), (5, 150, 1030, 4, 2, 64, 3, "interleaved"), (4, 300, 520, 4, 4, 32, 4, "modalities")],
+                         ids=lambda c: "x".join(map(str, c)))
+def test_cross_attend_many_rows(sn, case, dtype):
+    test_cross_attend(sn, case, dtype)
+
+
+def test_rising_scores_many_rows(sn):
+    for d in (16, 64):
+        for dtype in ("bf16", "f16"):
+            test_rising_scores(sn, dtype, 2000, 1500, d, 300.0)
+
+
+@pytest.mark.parametrize("d", [32, 128])
+def test_views_and_bad_heads_many_rows(sn, d):
+    B, Tq, Tk, Hq, Hk = 6, 300, 500, 4, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    kv = torch.randn((B, Tk, 2, Hk, d), generator=g, device="cuda").bfloat16()
+    q = torch.randn((2 * B, Tq, Hq, d), generator=g, device="cuda").bfloat16()
+    Q, K, V = q.transpose(1, 2)[::2], kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)
+    full = sn.cross_attend_fwd(Q, K, V)
+    assert torch.equal(full, sn.cross_attend_fwd(Q.contiguous(), K.contiguous(), V.contiguous()))
+    one = K[:1].expand(B, -1, -1, -1)
+    assert torch.equal(sn.cross_attend_fwd(Q, one, V), sn.cross_attend_fwd(Q, one.contiguous(), V))
+    kept = torch.tensor([[0, 1, 1, 1], [-1, 2, 3, 9], [0, 0, 0, 0], [3, 2, 1, 0], [4, 4, 4, 4], [2, 2, 3, 0]], dtype=torch.int32, device="cuda")
+    assert sn.last_status() == 0
+    O = sn.cross_attend_fwd(Q, K, V, kept, O=torch.full((B, 4, Tq, d), 3.0, dtype=torch.bfloat16, device="cuda"))
+    assert sn.last_status() == sentry.STATUS_BIT_BAD_INDEX
+    for b, row in enumerate(kept.tolist()):
+        for j, h in enumerate(row):
+            assert torch.equal(O[b, j], full[b, h] if 0 <= h < Hq else torch.zeros_like(O[b, j])), (b, j)
+
+
+def test_many_rows_of_a_cache_on_two_streams(sn):
+    """As test_prompts_on_two_streams, with calls that hold tensor memory."""
+    calls = [_cache_call(*s, seed=50 + i) for i, s in enumerate([(2, 300, 60, 32, 4, 2, 128), (3, 1, 300, 16, 8, 1, 128), (4, 400, 40, 64, 4, 1, 64)])]
+    alone = [sn.cache_attend_fwd(*c) for c in calls]
+    torch.cuda.synchronize()
+    other = sentry.Sentry(0)
+    try:
+        streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+        for i in range(24):
+            for s, st in zip((sn, other), streams):
+                with torch.cuda.stream(st):
+                    got.append((i % 3, s.cache_attend_fwd(*calls[i % 3])))
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, alone[i]) for i, o in got)
+        assert sn.last_status() == 0 and other.last_status() == 0
+    finally:
+        other.close()
