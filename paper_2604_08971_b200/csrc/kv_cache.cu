@@ -8,12 +8,11 @@
 
 #include <type_traits>
 
+#include "append_team.cuh"
 #include "serving.cuh"
 
 namespace {
 
-constexpr int kAppThreads = 256;
-constexpr int kHold = 8;
 constexpr int kAppPages = 4;      // of a block, at most
 
 __device__ __forceinline__ float nan_f32() { return __int_as_float(0x7fc00000); }
@@ -137,10 +136,9 @@ __global__ void __launch_bounds__(kAppThreads, 3) cache_append_kernel(const Appe
         s_id[threadIdx.x] = id;
     }
     __syncthreads();
-    // (K or V, head) of a page: `team` warps, so that a lane holds kHold pieces of 16 bytes at most (pages of fp32 may have twice that)
+    // (K or V, head) of a page: a team of warps
     const int shift = 31 - __clz(d / N), per_row = 1 << shift;       // pieces of a row
-    const int wide = (min(page, T_) << shift) / (32 * kHold), team = wide < 1 ? 1 : wide > kAppThreads / 32 ? kAppThreads / 32 : wide;
-    const int team_shift = 31 - __clz(team), lanes = 32 << team_shift, me = ((warp & (team - 1)) << 5) + lane;
+    const int team_shift = append_team_shift(page, T_, shift), team = 1 << team_shift, lanes = append_lanes(team_shift), me = append_place(warp, lane, team_shift);
     const int units = pages * 2 * Hk, at_a_time = (kAppThreads / 32) >> team_shift;
     for (int u0 = 0; u0 < units; u0 += at_a_time) {                  // (the same number of rounds for every warp)
         const int u = u0 + (warp >> team_shift), pi = u / (2 * Hk), unit = u - pi * 2 * Hk;
