@@ -518,8 +518,8 @@ SENTRY_API int sentry_linear_i8(sentry_ctx* ctx, const sentry_linear_desc* desc,
  * tensor; a token stride of 0 of K or V with Tk > 1 is UNSUPPORTED.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
  * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24, k_h * Tq < 2^30.
  * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (by 2^-8 and 2^-11 of
- * themselves at most), in the form for few rows as a rounded head and a remainder.  A row whose scores are all minus infinity
- * (from an infinite q or k) is zero.
+ * themselves at most; fp16 ones below 2^-21 of the row's largest by up to 2^-32 of that), in the form for few rows as a rounded
+ * head and a remainder, down to 2^-36 of the largest.  A row whose scores are all minus infinity (from an infinite q or k) is zero.
  * Workspace: sentry_cross_workspace_bytes.
  */
 typedef struct sentry_cross_desc {
@@ -585,8 +585,9 @@ SENTRY_API int sentry_cache_append(sentry_ctx* ctx, const sentry_kv_cache* cache
  * A row without a visible key is zero.  Lengths outside [0, max_pages * page] are clamped.
  * 16-bit Q meets the codes as fp16, each row scaled by a power of two so that its largest value lies in [1,2) (what the row has
  * below 2^-14 of it loses digits); the softmax weights are fp16 too, in the form for few rows as a head and a remainder where O
- * is fp16; all sums are fp32.  Value scales of the pages that a sample sees may differ by 2^64; values of pages smaller
- * yet lose digits.
+ * is fp16; all sums are fp32.  As for cross attention, with the products of a weight and its page's value scale in the place of the
+ * weights: what is small beside the largest of them loses digits.  Value scales of the pages that a sample sees may differ by 2^64; values of
+ * pages smaller yet lose digits.
  * e4m3 codes 0x7f and 0xff (NaN; sentry_cache_append writes none) give NaN.  Workspace: sentry_cache_workspace_bytes.
  */
 typedef struct sentry_cache_attend_desc {

@@ -10,9 +10,10 @@
 // shared memory through registers straight into the MMA: the order of the inner index is free as long as both operands share it, so that
 // a lane's 16 consecutive bytes of a key are its operand for K's product; and for V's, where pairs run along the keys, two keys'
 // words are interleaved byte by byte.  The weights get from the first product's layout to the second's by a transposition of 8 x 8
-// matrices among registers.  8-bit codes become fp16 exactly; a page's key scale multiplies the scores, its value scale the weights.
-// The maximum is followed only where a score exceeds it by 2^8.
-// One token of 32 samples of up to 4096 e4m3 tokens (16 heads on 4, d 128, 87 MB): 24 us, 3.6 TB/s over all; a block's first keys arrive 3.5 us
+// matrices among registers.  8-bit codes become fp16 exactly; a page's key scale multiplies the scores, the logarithm of its value scale is
+// added to them.  The maximum is followed only where a score exceeds it by 2^4 (fp16 weights) or 2^8 (bf16).
+// (Value scales that multiplied the weights, without the weights' 2^11, cost 0.6 us less here and lost small weights beside a large one.)
+// One token of 32 samples of up to 4096 e4m3 tokens (16 heads on 4, d 128, 87 MB): 25 us, 3.5 TB/s over all; a block's first keys arrive 3.5 us
 // after its start (lengths, page, keys: three loads that depend on one another), between that and the last tile the loads run at 5 to 5.7 TB/s,
 // and the parts meet in 3.  i8 of d 64 (2 x 131072 tokens, 67 MB): 29 us, where issue is as long as the bytes (640 instructions a warp for 32 keys).
 // Every wait is bounded; on expiry the block raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
@@ -184,6 +185,10 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
     constexpr bool DENSE = KV <= KV_F16, I8 = KV == KV_I8;
     constexpr bool MMA_BF16 = KV == KV_BF16;
     constexpr bool SPLIT_P = DENSE || !BF16;                 // weights as a head and a remainder
+    // The maximum is followed where a score exceeds it by 2^kLag.  fp16 weights are taken 2^kShift times as large (2^15 at most): its range is what
+    // small ones run out of, below 2^-25 of the largest weight (times its value scale), from where they round to multiples of 2^-35 of that.
+    // bf16 has fp32's range.
+    constexpr float kLag = MMA_BF16 ? 8.0f : 4.0f, kShift = MMA_BF16 ? 0.0f : 11.0f, kUnshift = MMA_BF16 ? 1.0f : 1.0f / 2048.0f;
     constexpr int KSTEPS = D / 16, DT = D / 16, ROWS = 8 * NT, RB = C::RB;
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned s_vis[C::STAGES];                   // keys of the slot's tile that are there
@@ -299,7 +304,7 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
                 if (++s == C::STAGES) { s = 0; ++use; }
             }
         }
-        float o[DT][NT][4], m[NT][2], l[NT][2], vref = 0.0f;        // O is in units of vref (8-bit values; see below)
+        float o[DT][NT][4], m[NT][2], l[NT][2], vref = 1.0f;        // O is in units of vref (8-bit values; see below)
         if (warp < kWarps) {
         uint32_t qf[NT][KSTEPS][2];
         float scale[NT][2];                                     // of rows 2 t4 and 2 t4 + 1, whose scores this lane will hold
@@ -377,33 +382,71 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
             for (int nt = 0; nt < NT; ++nt) all_see = min(all_see, min(last[nt][0], last[nt][1]));
             all_see = __reduce_min_sync(0xffffffffu, all_see);
         }
-        float inv_vref = 0.0f;
-        // scales of this warp's next 32 tiles, a lane each (of the first 16 keys and of the others; 0 where there is no page)
-        float ks0 = 1.0f, ks1 = 1.0f, vs0 = 1.0f, vs1 = 1.0f;
+        // A page's value scale goes into its keys' exponents, in units of the largest one of this warp's pages (vref): the maximum is then that of
+        // weight times scale, and no weight is lost whose values count.  The sum takes it out again.
+        // Key scales of this warp's next 32 tiles, a lane each (of the first 16 keys and of the others), logarithms and signs of the value scales.
+        // (A scale of 2^-100 of vref and less leaves zeros of its values; one that is no number makes them none.)
+        constexpr float kNoneLog = -99.99f;
+        float ks0 = 0.0f, ks1 = 0.0f, lg0 = 0.0f, lg1 = 0.0f;
+        unsigned odd0 = 0u, odd1 = 0u;                          // tiles with a scale below zero, or as good as zero
         int turn = 0;
+        auto pages_of = [&](int tile, int& id0, int& id1) {
+            const int32_t* pages = a.table + (size_t)b * a.max_pages;
+            const int mine = tile + lane * kWarps, n = mine * kKeys, shift = 31 - __clz(a.page);
+            id0 = id1 = mine < t1 ? pages[n >> shift] : -1;
+            if (shift == 4) id1 = mine < t1 && n + 16 < len ? pages[(n >> 4) + 1] : -1;
+            if ((unsigned)id0 >= (unsigned)a.n_pages) id0 = -1;
+            if ((unsigned)id1 >= (unsigned)a.n_pages) id1 = -1;
+        };
+        auto scale_of = [&](const float* scales, int id, float none) { return id >= 0 ? scales[(size_t)id * a.Hk + g] : none; };
+        auto size_of = [&](float vs) {                          // (as bits, which order sizes; what is no number counts as nothing)
+            const uint32_t v = __float_as_uint(vs) & 0x7fffffffu;
+            return v < 0x7f800000u ? v : 0u;
+        };
+        auto log_of = [&](float vs) { return fabsf(vs) <= 3.4028234e38f ? log2f(fmaxf(fabsf(vs) * (1.0f / vref), 7.8886091e-31f)) : __int_as_float(0x7fc00000); };
+        auto take = [&](int id0, int id1, float vs0, float vs1) {
+            ks0 = scale_of(a.k_scales, id0, 0.0f);
+            ks1 = scale_of(a.k_scales, id1, 0.0f);
+            lg0 = log_of(vs0);
+            lg1 = log_of(vs1);
+            odd0 = __ballot_sync(0xffffffffu, vs0 < 0.0f || lg0 <= kNoneLog);
+            odd1 = __ballot_sync(0xffffffffu, vs1 < 0.0f || lg1 <= kNoneLog);
+        };
+        if constexpr (!DENSE) {
+            int id0, id1;
+            pages_of(t0 + warp, id0, id1);
+            const float vs0 = scale_of(a.v_scales, id0, 0.0f), vs1 = scale_of(a.v_scales, id1, 0.0f);
+            uint32_t top = max(size_of(vs0), size_of(vs1));
+#pragma unroll 1
+            for (int tile = t0 + warp + 32 * kWarps; tile < t1; tile += 32 * kWarps) {
+                int far0, far1;
+                pages_of(tile, far0, far1);
+                top = max(top, max(size_of(scale_of(a.v_scales, far0, 0.0f)), size_of(scale_of(a.v_scales, far1, 0.0f))));
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            vref = top == 0u ? 1.0f : fmaxf(__uint_as_float(top), 7.5231638e-37f);     // (2^-120)
+            take(id0, id1, vs0, vs1);
+        }
 
         // -------------------------------------------------------------------- tiles of 32 keys
         for (int tile = t0 + warp; tile < t1; tile += kWarps) {
             const uint32_t n = done + (uint32_t)(tile - t0), slot = n % C::STAGES, parity = n / C::STAGES & 1;
             if constexpr (!DENSE) {
-                if (turn == 0) {
-                    const int32_t* pages = a.table + (size_t)b * a.max_pages;
-                    const int mine = tile + lane * kWarps, n = mine * kKeys, shift = 31 - __clz(a.page);
-                    int id0 = mine < t1 ? pages[n >> shift] : -1, id1 = id0;
-                    if (shift == 4) id1 = mine < t1 && n + 16 < len ? pages[(n >> 4) + 1] : -1;
-                    ks0 = ks1 = vs0 = vs1 = 0.0f;
-                    if ((unsigned)id0 < (unsigned)a.n_pages) { ks0 = a.k_scales[(size_t)id0 * a.Hk + g]; vs0 = a.v_scales[(size_t)id0 * a.Hk + g]; }
-                    if ((unsigned)id1 < (unsigned)a.n_pages) { ks1 = a.k_scales[(size_t)id1 * a.Hk + g]; vs1 = a.v_scales[(size_t)id1 * a.Hk + g]; }
+                if (turn == 0 && tile >= t0 + kWarps) {
+                    int id0, id1;
+                    pages_of(tile, id0, id1);
+                    take(id0, id1, scale_of(a.v_scales, id0, 0.0f), scale_of(a.v_scales, id1, 0.0f));
                 }
             }
             if (!warp_wait(&s_kfull[slot], parity, abort_flag)) break;
             const int n0 = tile * kKeys;
             const uint32_t kt = ring + slot * 2 * C::TILE, vt = kt + C::TILE;
             const unsigned vis = s_vis[slot];
-            float kscale[2] = {1.0f, 1.0f}, vscale[2] = {1.0f, 1.0f};
+            float kscale[2] = {1.0f, 1.0f}, vlog[2] = {0.0f, 0.0f};
+            const int now = turn;
             if constexpr (!DENSE) {
-                kscale[0] = __shfl_sync(0xffffffffu, ks0, turn); kscale[1] = __shfl_sync(0xffffffffu, ks1, turn);
-                vscale[0] = __shfl_sync(0xffffffffu, vs0, turn); vscale[1] = __shfl_sync(0xffffffffu, vs1, turn);
+                kscale[0] = __shfl_sync(0xffffffffu, ks0, now); kscale[1] = __shfl_sync(0xffffffffu, ks1, now);
+                vlog[0] = __shfl_sync(0xffffffffu, lg0, now); vlog[1] = __shfl_sync(0xffffffffu, lg1, now);
                 turn = (turn + 1) & 31;
             }
             const bool any = __any_sync(0xffffffffu, vis != 0), full = __all_sync(0xffffffffu, vis == 0xffffffffu && n0 + kKeys <= all_see);
@@ -443,7 +486,7 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
                     for (int nt = 0; nt < NT; ++nt) {
                         const float c0 = scale[nt][0] * ks, c1 = scale[nt][1] * ks;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) s[mt][nt][x] *= x & 1 ? c1 : c0;
+                        for (int x = 0; x < 4; ++x) s[mt][nt][x] = DENSE ? s[mt][nt][x] * (x & 1 ? c1 : c0) : fmaf(s[mt][nt][x], x & 1 ? c1 : c0, vlog[mt]);
                     }
                 }
             }
@@ -468,7 +511,7 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const float top = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
-                        over = over || top - m[nt][x] > 8.0f;
+                        over = over || top - m[nt][x] > kLag;
                     }
                 if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -480,7 +523,7 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
 #pragma unroll
                             for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
                             // (each row for itself: what its neighbours hold changes no bit of it)
-                            const bool grew = top - m[nt][x] > 8.0f;
+                            const bool grew = top - m[nt][x] > kLag;
                             keep[x] = grew ? exp2_fast(m[nt][x] - top) : 1.0f;
                             m[nt][x] = grew ? top : m[nt][x];
                             l[nt][x] *= keep[x];
@@ -493,51 +536,35 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const float ref[2] = {m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m[nt][1] == -INFINITY ? 0.0f : m[nt][1]};
+                    const float ref[2] = {(m[nt][0] == -INFINITY ? 0.0f : m[nt][0]) - kShift, (m[nt][1] == -INFINITY ? 0.0f : m[nt][1]) - kShift};
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt)
+                    for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            s[mt][nt][x] = exp2_fast(s[mt][nt][x] - ref[x & 1]);
-                            l[nt][x & 1] += s[mt][nt][x];
+                        for (int x = 0; x < 4; ++x) s[mt][nt][x] = exp2_fast(s[mt][nt][x] - ref[x & 1]);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float sum = s[mt][nt][x] + s[mt][nt][x + 2];
+                            if constexpr (DENSE) l[nt][x] += sum;
+                            else {
+                                // a weight counts in the sum without its page's value scale (which may be no number, where a row sees nothing of the page)
+                                const float out = exp2_fast(-vlog[mt]);
+                                l[nt][x] = full || sum != 0.0f ? fmaf(sum, out, l[nt][x]) : l[nt][x];
+                            }
                         }
+                    }
                 }
                 if (!warp_wait(&s_vfull[slot], parity, abort_flag)) break;
                 // ------ values, 16 keys at a time: column gq * (D / 8) + 2 j is row gq of the MMA's tile j, the next column its row gq + 8
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
                     if constexpr (!DENSE) {
-                        // The page's scale multiplies the weights, as a ratio to vref; where it is far from that, O changes its unit.
-                        // (A page 2^64 times smaller leaves it: its values are nothing beside what O may hold.)
                         if (!full && ((vis >> (kk * 16)) & 0xffffu) == 0) continue;
-                        const float vs = vscale[kk];
-                        float ratio = vs * inv_vref;
-                        if (!(fabsf(ratio) >= 0.0625f && fabsf(ratio) <= 16.0f)) {
-                            if (!(fabsf(vs) <= 3.4028234e38f)) ratio = __int_as_float(0x7fc00000);
-                            else if (fabsf(vs) >= fmaxf(1.17549435e-38f, fabsf(vref) * 5.42101086e-20f)) {
-                                const float f = vref / vs;
-#pragma unroll
-                                for (int j = 0; j < DT; ++j)
-#pragma unroll
-                                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                        for (int x = 0; x < 4; ++x) o[j][nt][x] *= f;
-                                vref = vs;
-                                inv_vref = 1.0f / vs;
-                                ratio = 1.0f;
-                            }
-                        }
-                        if (full) {
+                        if ((kk ? odd1 : odd0) >> now & 1u) {
+                            const float f = __shfl_sync(0xffffffffu, kk ? lg1 : lg0, now) <= kNoneLog ? 0.0f : -1.0f;
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) s[kk][nt][x] *= ratio;
-                        } else {
-                            // (a row that sees nothing of the page takes nothing of its scale, which may not be a number)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) s[kk][nt][x] = s[kk][nt][x] != 0.0f ? s[kk][nt][x] * ratio : 0.0f;
+                                for (int x = 0; x < 4; ++x) s[kk][nt][x] *= f;
                         }
                     }
                     uint32_t p[NT][2], q[NT][2];
@@ -623,11 +650,11 @@ kv_rows_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const 
                 const int r = nt * 8 + 2 * t4 + x;
 #pragma unroll
                 for (int y = 4; y < 32; y <<= 1) l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], y);
-                if (gq == 0) { s_m[warp][r] = m[nt][x]; s_l[warp][r] = l[nt][x]; }
+                if (gq == 0) { s_m[warp][r] = m[nt][x]; s_l[warp][r] = l[nt][x] * kUnshift; }
 #pragma unroll
                 for (int j = 0; j < DT; ++j) {
-                    const float f = DENSE ? 1.0f : vref;
-                    *reinterpret_cast<float2*>(so + (warp * ROWS + r) * D + gq * (D / 8) + 2 * j) = make_float2(o[j][nt][x] * f, o[j][nt][x + 2] * f);
+                    // (first one, then the other: large values have room, and vref may be as small as numbers get)
+                    *reinterpret_cast<float2*>(so + (warp * ROWS + r) * D + gq * (D / 8) + 2 * j) = make_float2(o[j][nt][x] * kUnshift * vref, o[j][nt][x + 2] * kUnshift * vref);
                 }
             }
         }

@@ -50,3 +50,80 @@ def test_append_short_prompts(sn, fmt, dtype, Hk, page, d, T):
             np.testing.assert_array_equal(dev[2 * i + 1].cpu().numpy(), s)
             np.testing.assert_array_equal(dev[2 * i].cpu().numpy(), c)
     assert sn.last_status() == 0
+
+
+# ------------------------------------------------------------------------------------------ small weights beside a large one
+
+def _strong(rng, N, d, below, at):
+    """q [d] and k [N,d] whose weights are 2^-below of the strong ones' at keys `at`, half a power of two up and down."""
+    q = np.where(np.arange(d) % 2, 1.0, -1.0)
+    k = rng.uniform(-0.5, 0.5, N) * np.log(2)
+    k[at] = below * np.log(2)
+    return q, (k / np.sqrt(d))[:, None] * q
+
+
+def _check_alike(O, q, k, v, dtype, weight_err):
+    """Every row of O against the same one; a sink's values leave nothing but the small weights'."""
+    want, tol = ref.attention(q[None], k, v, np.ones((1, k.shape[0]), bool), dtype, weight_err)
+    rows = O.detach().cpu().double().numpy().reshape(-1, q.shape[0])
+    ref.check(rows, np.broadcast_to(want, rows.shape), np.broadcast_to(tol, rows.shape))
+
+
+# Samples enough that no axis of keys is split, so that every small weight meets a strong one: every fourth tile of 32 keys goes to the same warp.
+AT = [3, 40, 77, 100]
+FEW, MANY = (600, 1), (160, 300)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("sink", [True, False])
+@pytest.mark.parametrize("below", [16.3, 20.6, 24.4])
+@pytest.mark.parametrize("B,Tq,N,d", [FEW + (8200, 64), MANY + (8200, 64), FEW + (5003, 128), MANY + (5003, 128), FEW + (3001, 32), (1, 1, 3001, 64)])
+def test_small_weights_cross(sn, dtype, sink, below, B, Tq, N, d):
+    """fp16 weights are good to half a step, 2^-11 of themselves, down to 2^-25 of a row's largest."""
+    if dtype == "f32":
+        B = 2
+    rng = np.random.default_rng(N)
+    q, k = _strong(rng, N, d, below, AT)
+    v = rng.uniform(0.5, 1.5, (N, d))
+    v[AT] = 0.0 if sink else 1.0
+    Q = torch.from_numpy(q).to(DT[dtype]).expand(B, 1, Tq, d).contiguous()
+    K, V = (torch.from_numpy(x).to(DT[dtype])[None, None] for x in (k, v))
+    O = sn.cross_attend_fwd(Q.cuda(), K.cuda().expand(B, 1, N, d), V.cuda().expand(B, 1, N, d))
+    assert sn.last_status() == 0
+    weight_err = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 0.0}[dtype]
+    _check_alike(O, q, K[0, 0].double().numpy(), V[0, 0].double().numpy(), DT[dtype], weight_err)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("sink", [True, False])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("below,times", [(16.3, 1), (24.4, 1), (16.3, 16), (20.4, 16), (20.4, 1.0 / 16), (14.4, 1024)])
+@pytest.mark.parametrize("B,Tq,N,d,page", [FEW + (8200, 64, 32), MANY + (8200, 64, 32), FEW + (5003, 128, 16), MANY + (5003, 128, 64), (1, 1, 3001, 64, 16)])
+def test_small_weights_cache(sn, dtype, sink, fmt, below, times, B, Tq, N, d, page):
+    """The same on a cache, for the product of a weight and its page's value scale: the strong keys' pages have `times` the others' scale."""
+    if dtype == "f32":
+        B = 2
+    rng = np.random.default_rng(N)
+    cols = -(-N // page)
+    q, k = _strong(rng, N, d, below, AT)
+    code = (lambda x: x.astype(np.int8)) if fmt == "i8" else ref.to_e4m3
+    strong = np.array(sorted({n // page for n in AT}))
+    # (keys that share a strong one's page have coarse codes: the scores are what the codes say)
+    ks = np.full((cols, 1), np.abs(k[np.setdiff1d(np.arange(N), AT)]).max() / (100 if fmt == "i8" else 400), np.float32)
+    ks[strong] = np.float32(np.abs(k).max() / (127 if fmt == "i8" else 448))
+    vs = np.full((cols, 1), 0.01, np.float32)
+    vs[strong] *= times
+    pad = np.zeros((cols * page, d))
+    pad[:N] = k
+    kc = code(np.rint(pad / np.repeat(ks, page, 0)) if fmt == "i8" else pad / np.repeat(ks, page, 0)).reshape(cols, 1, page, d)
+    v = rng.integers(32, 127, (cols * page, d)).astype(float)
+    for p in strong:                                          # values of the strong keys' page: what its scale makes large is the strong key's alone
+        v[p * page:(p + 1) * page] = 0.0
+    v[AT] = 0.0 if sink else 100.0
+    vc = code(v).reshape(cols, 1, page, d)
+    table = np.broadcast_to(np.arange(cols, dtype=np.int32), (B, cols)).copy()
+    Q = torch.from_numpy(q).to(DT[dtype]).expand(B, 1, Tq, d).contiguous()
+    O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, np.full(B, N, np.int32)))
+    assert sn.last_status() == 0
+    kk, vv = ((ref.values(c, fmt) * s[..., None, None].astype(np.float64)).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
+    _check_alike(O, q, kk, vv, DT[dtype], 2.0 ** -11 if dtype != "f32" else 0.0)
