@@ -518,8 +518,8 @@ SENTRY_API int sentry_linear_i8(sentry_ctx* ctx, const sentry_linear_desc* desc,
  * tensor; a token stride of 0 of K or V with Tk > 1 is UNSUPPORTED.  d in {16,32,64,128}; Hq % Hk == 0, Hq <= 256,
  * Tq, Tk >= 0 below 2^24, B >= 0, B * Hq < 2^24, k_h * Tq < 2^30.
  * Scores, sums and accumulators are fp32; the softmax weights meet 16-bit V rounded to V's type (by 2^-8 and 2^-11 of
- * themselves at most; fp16 ones below 2^-21 of the row's largest by up to 2^-32 of that), in the form for few rows as a rounded
- * head and a remainder, down to 2^-36 of the largest.  A row whose scores are all minus infinity (from an infinite q or k) is zero.
+ * themselves at most; fp16 ones below 2^-25 of the row's largest by up to 2^-36 of that), in the form for few rows as a rounded
+ * head and a remainder.  A row whose scores are all minus infinity (from an infinite q or k) is zero.
  * Workspace: sentry_cross_workspace_bytes.
  */
 typedef struct sentry_cross_desc {

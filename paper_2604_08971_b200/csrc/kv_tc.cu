@@ -6,8 +6,8 @@
 //                        the scores that it has read
 //   O_t += P_t V         tcgen05, P from tensor memory, V as it lies in memory (MN-major)
 // Two tiles, so that the tensor core works for one while the other's rows are exponentiated.  The accumulator follows the running maximum
-// only where it grew by more than 2^8: until then weights are up to 2^8 instead of 1, which costs neither range nor precision, and
-// almost no iteration touches O.
+// only where it grew by more than 2^8 (bf16 weights) or 2^4 (fp16): until then weights are that much larger than 1, for which there is
+// range, and almost no iteration touches O.
 //
 // Bound by the exponentials (16 a clock and SM) up to d 64, by those and the products together at d 128.  Up to d 64 a step is of 64 keys and
 // an SM holds two CTAs, four tiles that wait for one another's latencies (4 x 4096 rows on 8192 keys, 16 heads on 4, d 64, bf16: 830 us, against
@@ -198,7 +198,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
     const int tiles = (count + KN - 1) / KN, per_split = (tiles + n_splits - 1) / n_splits;
     const int t0 = min(split * per_split, tiles), t1 = min(t0 + per_split, tiles);
     // A page's value scale goes into its keys' exponents, so that O needs no unit that follows the pages: in units of the largest one of this
-    // CTA's pages (vref), and 2^-100 of it at least.
+    // CTA's pages (vref).  (2^-100 of it and less leaves zeros of the page's values.)
     float vref = 1.0f;
     const int page_shift = CODES ? 31 - __clz(a.page) : 0;
     if constexpr (CODES) {
@@ -325,7 +325,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     fetch(kv, a.K, j + 1, then.id);
                     ok = warp_wait(&misc->v_empty[s], (use & 1) ^ 1, abort_flag);
                     if (!ok) break;
-                    convert(vv, v_smem + s * C::KTILE, now.id < 0 ? 0 : now.vs == 0.0f ? -1 : now.vs < 0.0f);
+                    convert(vv, v_smem + s * C::KTILE, now.id < 0 ? 0 : fabsf(now.vs) * inv_vref <= 7.8886091e-31f ? -1 : now.vs < 0.0f);
                     warp_arrive(&misc->v_full[s]);
                     fetch(vv, a.V, j + 1, then.id);
                     now = then;
@@ -453,8 +453,9 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 if (BF16) cq *= misc->c.q_scale[t * kTM + (warp & 3) * 32 + lane];
                 if (a.causal) last = min(count, count - a.Tq + row % a.Tq + 1);
             }
-            // fp16 weights are taken 2^7 times as large (2^15 at most): its range is what small ones run out of
-            constexpr float kShift = OP_BF16 ? 0.0f : 7.0f;
+            // The maximum is followed where a score exceeds it by 2^kLag.  fp16 weights are taken 2^kShift times as large (2^15 at most): its range is
+            // what small ones run out of, below 2^-25 of the largest (times its value scale), from where they round to multiples of 2^-35 of that.
+            constexpr float kLag = OP_BF16 ? 8.0f : 4.0f, kShift = OP_BF16 ? 0.0f : 11.0f, kUnshift = OP_BF16 ? 1.0f : 1.0f / 2048.0f;
             float m = -INFINITY, l = 0.0f;
             bool ok = true;
             for (int j = 0; j < steps && ok && t < halves; ++j) {
@@ -522,7 +523,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 const float now = max3_nan(max3_nan(m, top[0], top[1]), top[2], top[3]);
                 if (j == 0) m = now;
                 else {
-                    const bool grew = !((now - m) * cm <= 8.0f);
+                    const bool grew = !((now - m) * cm <= kLag);
                     if (__any_sync(0xffffffffu, grew)) {
                         // O follows the maximum; the last product into it has to be complete
                         ok = warp_wait(&misc->o_full[t], (n - 1) & 1, abort_flag);
@@ -591,7 +592,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                 const size_t each = (size_t)a.k_h * a.Tq, within = in ? (size_t)misc->pos[row / a.Tq] * a.Tq + row % a.Tq : 0;
                 const size_t out = b * each + within, pat = ((size_t)b * n_splits + split) * each + within;
                 const float inv = l == 0.0f ? 0.0f : vref / l;
-                if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * cm - kShift, l) : make_float2(-INFINITY, 0.0f);
+                if (n_splits > 1 && in) ml[pat] = steps > 0 ? make_float2(m * cm, l * kUnshift) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
                 for (int z = 0; z < D; z += 16) {
                     uint32_t o[16];
@@ -613,7 +614,7 @@ kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvAttendArgs a, const in
                     } else if (steps > 0) {
                         uint4* dst = reinterpret_cast<uint4*>(part + pat * D + z);
 #pragma unroll
-                        for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * vref);
+                        for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * kUnshift * vref);     // (large values have room)
 #pragma unroll
                         for (int y = 0; y < 4; ++y) dst[y] = make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
                     }

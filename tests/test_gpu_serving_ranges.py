@@ -127,3 +127,41 @@ def test_small_weights_cache(sn, dtype, sink, fmt, below, times, B, Tq, N, d, pa
     assert sn.last_status() == 0
     kk, vv = ((ref.values(c, fmt) * s[..., None, None].astype(np.float64)).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
     _check_alike(O, q, kk, vv, DT[dtype], 2.0 ** -11 if dtype != "f32" else 0.0)
+
+
+# (all small weights alike, so that they round alike; several sizes, since one may happen to be a number of the type)
+EQUAL = [21.23, 22.41, 23.17, 23.77, 24.37]
+
+
+@pytest.mark.parametrize("below", EQUAL)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B,Tq,N,d", [MANY + (8200, 64), MANY + (5003, 128), (2, 300, 5003, 128), FEW + (8200, 64)])
+def test_equal_small_weights_cross(sn, dtype, below, B, Tq, N, d):
+    q, k = _strong(np.random.default_rng(N), N, d, below, AT)
+    k[np.setdiff1d(np.arange(N), AT)] = 0.0
+    v = np.ones((N, d))
+    v[AT] = 0.0
+    Q = torch.from_numpy(q).to(DT[dtype]).expand(B, 1, Tq, d).contiguous()
+    K, V = (torch.from_numpy(x).to(DT[dtype])[None, None] for x in (k, v))
+    O = sn.cross_attend_fwd(Q.cuda(), K.cuda().expand(B, 1, N, d), V.cuda().expand(B, 1, N, d))
+    _check_alike(O, q, K[0, 0].double().numpy(), V[0, 0].double().numpy(), DT[dtype], 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11)
+
+
+@pytest.mark.parametrize("below", EQUAL)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("B,Tq,N,d,page", [MANY + (8200, 64, 32), MANY + (5003, 128, 64), (2, 600, 5003, 128, 64), FEW + (8200, 64, 32)])
+def test_equal_small_weights_cache(sn, dtype, fmt, below, B, Tq, N, d, page):
+    q, _ = _strong(np.random.default_rng(N), N, d, below, AT)
+    cols, top = -(-N // page), 127 if fmt == "i8" else 448
+    k, v = np.zeros((cols * page, d)), np.full((cols * page, d), 96.0)
+    k[AT] = top * q
+    v[AT] = 0.0
+    code = (lambda x: x.astype(np.int8)) if fmt == "i8" else ref.to_e4m3
+    kc, vc = (code(x).reshape(cols, 1, page, d) for x in (k, v))
+    ks, vs = np.full((cols, 1), below * np.log(2) / np.sqrt(d) / top, np.float32), np.full((cols, 1), 0.01, np.float32)
+    table = np.broadcast_to(np.arange(cols, dtype=np.int32), (B, cols)).copy()
+    Q = torch.from_numpy(q).to(DT[dtype]).expand(B, 1, Tq, d).contiguous()
+    O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, np.full(B, N, np.int32)))
+    kk, vv = ((ref.values(c, fmt) * s[..., None, None].astype(np.float64)).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
+    _check_alike(O, q, kk, vv, DT[dtype], 2.0 ** -11)
