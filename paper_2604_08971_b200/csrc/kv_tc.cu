@@ -750,8 +750,8 @@ size_t kv_tc_ws_bytes(const KvAttendArgs& a) {
     const size_t rows = (size_t)a.B * a.k_h * a.Tq;
     size_t bytes = 0;
     if (n > 1) bytes += align_up(n * rows * a.d * sizeof(float), 256) + align_up(n * rows * sizeof(float2), 256);
-    if (a.Tk <= kTcListed) return bytes + 512;
-    // (whether the call has modality ids is not in the descriptor)
+    if (a.format != 0 || a.Tk <= kTcListed) return bytes + 512;        // (a cache has no modality ids)
+    // (whether a dense call has some is not in the descriptor)
     return bytes + align_up((size_t)a.B * a.Tk * sizeof(int32_t), 256) + align_up((size_t)a.B * sizeof(int32_t), 256) + 512;
 }
 int launch_kv_tc(sentry_ctx* ctx, const KvAttendArgs& a, WsAlloc& ws, cudaStream_t st) {
