@@ -7,6 +7,7 @@
 
 #include <type_traits>
 
+#include "linear_tiles.cuh"
 #include "serving.cuh"
 #include "tc_common.cuh"
 
@@ -80,7 +81,7 @@ int launch_quantize(sentry_ctx* ctx, int M, int K, const void* X, int8_t* codes,
     const bool one = (long long)M >= 8LL * ctx->sm_count && pieces <= 32 * 8;
     auto k = one ? (pieces <= 64 ? quantize_rows_kernel<T, 1, 2> : pieces <= 128 ? quantize_rows_kernel<T, 1, 4> : quantize_rows_kernel<T, 1, 8>)
                  : (pieces <= 256 ? quantize_rows_kernel<T, 8, 1> : quantize_rows_kernel<T, 8, 8>);
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(one ? (M + 7) / 8 : M)), dim3(256), 0, st, (const T*)X, codes, scales, M, K));
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)(one ? linear_tiles(M, 8) : M)), dim3(256), 0, st, (const T*)X, codes, scales, M, K));
     return SENTRY_OK;
 }
 
@@ -149,7 +150,7 @@ int launch_few(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
     auto k = tiles <= 1 ? linear_i8_few_kernel<T, 1> : tiles <= 2 ? linear_i8_few_kernel<T, 2> : tiles <= 4 ? linear_i8_few_kernel<T, 4>
                                                                                                              : linear_i8_few_kernel<T, 8>;
     LaunchScope ls(ctx, KS_LINEAR, st);
-    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)((a.d.N + 15) / 16)), dim3(256), 0, st, a.X, a.W, a.xs, a.ws, a.bias, (T*)a.Y, M, a.d.K, a.d.N));
+    SENTRY_CUDA_TRY(launch_chained(k, dim3((unsigned)linear_tiles(a.d.N, 16)), dim3(256), 0, st, a.X, a.W, a.xs, a.ws, a.bias, (T*)a.Y, M, a.d.K, a.d.N));
     return SENTRY_OK;
 }
 
@@ -261,8 +262,8 @@ linear_i8_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
     ptx::tc_fence_after_sync();
     const uint32_t tmem = misc->tmem_base;
     grid_dependency_wait();
-    const int n_tiles = (N + BN - 1) / BN;
-    const long long tiles = (long long)n_tiles * ((M + 128 * P - 1) / (128 * P));
+    const int n_tiles = (int)linear_tiles(N, BN);
+    const long long tiles = n_tiles * linear_tiles(M, 128 * P);
     const long long tile0 = blockIdx.x / P, tile_step = gridDim.x / P;
     const int KB = (K + 127) / 128;
 
@@ -453,7 +454,7 @@ int launch_tc(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
     CUtensorMap mx, mw, my = {};
     if (!make_map_i8(&mx, a.X, a.d.M, a.d.K, 128) || !make_map_i8(&mw, a.W, a.d.N, a.d.K, C::B_ROWS)) return SENTRY_ERR_CUDA;
     if (a.d.N % (16 / (int)sizeof(T)) == 0 && !make_map_out<T>(&my, a.Y, a.d.M, a.d.N)) return SENTRY_ERR_CUDA;
-    const long long tiles = (long long)((a.d.M + 128 * P - 1) / (128 * P)) * ((a.d.N + BN - 1) / BN), most = ctx->sm_count / P;
+    const long long tiles = linear_tiles(a.d.M, 128 * P) * linear_tiles(a.d.N, BN), most = ctx->sm_count / P;
     auto k = linear_i8_tc_kernel<T, P, BN>;
     static std::atomic<unsigned long long> allowed{0};
     SENTRY_CUDA_TRY(allow_smem(k, C::SMEM, ctx->device, allowed));
@@ -467,7 +468,7 @@ template <typename T>
 int launch_linear(sentry_ctx* ctx, const LinearArgs& a, cudaStream_t st) {
     if (a.d.M <= 64) return launch_few<T>(ctx, a, st);
     // pairs where their tiles fill the GPU; else narrower tiles, so that more SMs have one
-    auto tiles = [&](long long m, long long n) { return ((a.d.M + m - 1) / m) * ((a.d.N + n - 1) / n); };
+    auto tiles = [&](int m, int n) { return linear_tiles(a.d.M, m) * linear_tiles(a.d.N, n); };
     if (2 * tiles(256, 256) >= ctx->sm_count) return launch_tc<T, 2, 256>(ctx, a, st);
     return 2 * tiles(128, 128) >= ctx->sm_count ? launch_tc<T, 1, 128>(ctx, a, st) : launch_tc<T, 1, 64>(ctx, a, st);
 }

@@ -165,3 +165,21 @@ def test_equal_small_weights_cache(sn, dtype, fmt, below, B, Tq, N, d, page):
     O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, np.full(B, N, np.int32)))
     kk, vv = ((ref.values(c, fmt) * s[..., None, None].astype(np.float64)).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
     _check_alike(O, q, kk, vv, DT[dtype], 2.0 ** -11)
+
+
+def test_linear_of_the_most_rows(sn):
+    """2^31 - 1 rows: the last tile ends where 32 bits do."""
+    M, K = 2 ** 31 - 1, 16
+    if torch.cuda.mem_get_info()[0] < 70 << 30:
+        pytest.skip("needs 70 GB")
+    x, xs = torch.ones((M, K), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda")
+    rows = [0, 255, 256, 2 ** 30, M - 256, M - 2, M - 1]
+    for i, r in enumerate(rows):
+        x[r] = i + 2
+    w, ws = torch.ones((1, K), dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    Y = sn.linear_i8(x, xs, w, ws)
+    assert sn.last_status() == 0 and Y.shape == (M, 1)
+    assert [Y[r, 0].item() for r in rows] == [16.0 * (i + 2) for i in range(len(rows))]
+    assert int((Y == 16).sum()) == M - len(rows)
+    del x, xs, Y
+    torch.cuda.empty_cache()
