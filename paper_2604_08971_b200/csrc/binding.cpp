@@ -12,6 +12,7 @@
 #include <Python.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -68,8 +69,9 @@ T* ptr(PyObject* o) {
     return o == Py_None ? nullptr : ptr<T>(tensor(o));
 }
 // The caller's output, or a fresh one beside `like` (from native code: half the time of torch.empty; without the dispatcher, a quarter).
+// A dispatch mode sees the allocation: with one, it goes through the dispatcher.
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
-    if (like.is_cuda()) return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
+    if (like.is_cuda() && !c10::impl::TorchDispatchModeTLS::any_modes_set()) return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
     return at::empty(shape, like.options().dtype(type));
 }
 at::Tensor output(PyObject* o, at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {

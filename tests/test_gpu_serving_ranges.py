@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 import torch
+from torch.utils._python_dispatch import TorchDispatchMode
 
 import paper_2604_08971_b200 as sentry
 from tests import serving_reference as ref
@@ -183,3 +184,30 @@ def test_linear_of_the_most_rows(sn):
     assert int((Y == 16).sum()) == M - len(rows)
     del x, xs, Y
     torch.cuda.empty_cache()
+
+
+class _Allocations(TorchDispatchMode):
+    def __init__(self):
+        super().__init__()
+        self.shapes = []
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        if func._schema.name == "aten::empty":
+            self.shapes.append(tuple(args[0]))
+        return func(*args, **(kwargs or {}))
+
+
+def test_dispatch_modes_see_outputs(sn):
+    """A mode that watches allocations sees the outputs that the calls make, and changes none of them."""
+    scores, masks = torch.rand((8, 40), device="cuda"), torch.arange(8, dtype=torch.int32, device="cuda")
+    x, w = torch.randn((6, 64), device="cuda").bfloat16(), torch.randn((5, 64), device="cuda")
+    Q, K = torch.randn((2, 4, 3, 32), device="cuda").half(), torch.randn((2, 2, 7, 32), device="cuda").half()
+    calls = [(lambda: [sn.gate_select(scores, masks, 9)], [(8, 9)]), (lambda: list(sn.quantize_rows_i8(x)), [(6, 64), (6,)]),
+             (lambda: [sn.linear_i8(*codes, *weights)], [(6, 5)]), (lambda: [sn.cross_attend_fwd(Q, K, K)], [(2, 4, 3, 32)])]
+    codes, weights = sn.quantize_rows_i8(x), sn.quantize_rows_i8(w)
+    for call, shapes in calls:
+        want = call()
+        with _Allocations() as mode:
+            got = call()
+        assert mode.shapes == shapes
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
