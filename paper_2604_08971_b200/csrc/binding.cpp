@@ -443,7 +443,8 @@ struct Serving {
         stride[0] = stride[1] = stride[2] = 0;
         if (t.is_contiguous()) return t.data_ptr();
         if (t.size(3) > 1 && t.stride(3) != 1) refuse("the last dimension has to be contiguous");
-        for (int i = 0; i < 3; ++i) stride[i] = t.size(i) > 1 ? t.stride(i) : t.size(1) * t.size(2) * t.size(3);
+        // (a dimension of size one has any stride: one that is allowed, however far the others reach)
+        for (int i = 0; i < 3; ++i) stride[i] = t.size(i) > 1 ? t.stride(i) : t.size(3);
         if (stride[0] == 0 && stride[1] == 0 && stride[2] == 0) refuse("a tensor that is expanded along every dimension");
         return t.data_ptr();
     }

@@ -211,3 +211,20 @@ def test_dispatch_modes_see_outputs(sn):
             got = call()
         assert mode.shapes == shapes
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_sample_of_shared_heads(sn, dtype):
+    """One tensor for every head of one sample: what the heads' keys would take if each had its own is no limit."""
+    H, T, d, n = 256, (1 << 23) + 8, 128, 100
+    q, one = torch.randn((1, H, 1, d), device="cuda").to(DT[dtype]), torch.empty((1, 1, T, d), dtype=DT[dtype], device="cuda")
+    one[:, :, :n] = torch.randn((n, d), device="cuda")
+    K, lengths = one.expand(1, H, T, d), torch.tensor([n], dtype=torch.int32, device="cuda")
+    O = sn.cross_attend_fwd(q, K, K, key_lengths=lengths)
+    k = one[0, 0, :n].double().cpu().numpy()
+    for h in (0, 100, 255):
+        want, tol = ref.attention(q[0, h].double().cpu().numpy(), k, k, np.ones((1, n), bool), DT[dtype], 2.0 ** -8 if dtype == "bf16" else 0.0)
+        ref.check(O[0, h].double().cpu().numpy(), want, tol)
+    assert sn.last_status() == 0
+    del one, K
+    torch.cuda.empty_cache()
