@@ -19,10 +19,11 @@
 // Every wait is bounded; on expiry the block raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"
+#include "kv_rows_ring.cuh"
 
 namespace {
 
-constexpr int kWarps = 4, kKeys = 32, kRowsThreads = (kWarps + 1) * 32;
+constexpr int kWarps = kRowsWarps, kKeys = kRowsKeys, kRowsThreads = (kWarps + 1) * 32;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2, KV_I8 = 3 };
@@ -33,8 +34,9 @@ struct RowsCfg {
     static constexpr int ROW = D * ESIZE;                    // bytes of a key
     static constexpr int RB = ROW < 128 ? ROW : 128;         // of a row in shared memory; wider keys lie in slabs
     static constexpr int TILE = kKeys * ROW < 1024 ? 1024 : kKeys * ROW;   // of K or V, on the swizzle's boundary
-    // tiles of the ring (two for each warp at least, but for 16-bit rows of 128), and blocks on an SM
-    static constexpr int STAGES = TILE > 4096 ? 6 : TILE > 2048 ? 8 : 12;
+    // tiles of the ring, and blocks on an SM
+    static constexpr int STAGES = rows_stages(TILE);
+    static_assert(STAGES % kWarps == 0, "a slot is one warp's");
     static constexpr int BLOCKS = TILE > 4096 ? 2 : TILE > 2048 ? 3 : 4;
     static constexpr int RING = STAGES * 2 * TILE;
     static constexpr int MERGE = kWarps * 16 * D * 4;

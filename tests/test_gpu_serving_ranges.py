@@ -228,3 +228,43 @@ def test_one_sample_of_shared_heads(sn, dtype):
     assert sn.last_status() == 0
     del one, K
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------ keys from memory rather than the L2
+
+# B, Tq, N, Hq, Hk, d, k_h, runs of one modality
+FAR = [(17, 1, 7961, 21, 3, 128, 21, 900), (64, 1, 3424, 8, 2, 128, 4, 1200), (64, 2, 2979, 14, 2, 128, 7, 20), (64, 2, 7874, 16, 4, 128, 16, 0), (3, 5, 60001, 4, 1, 128, 4, 33),
+       (64, 1, 5995, 16, 4, 64, 8, 700), (64, 2, 9001, 14, 2, 32, 7, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", FAR, ids=lambda c: "x".join(map(str, c)))
+def test_cross_attend_keys_beyond_the_l2(sn, case, dtype):
+    """Copies that land late and out of order: the same bits five times, and the definition's values."""
+    B, Tq, N, Hq, Hk, d, k_h, run = case
+    g, rng = torch.Generator(device="cuda").manual_seed(N), np.random.default_rng(N)
+    kv = torch.randn((B, N, 2, Hk, d), generator=g, device="cuda", dtype=DT[dtype])
+    Q = torch.randn((B, Hq, Tq, d), generator=g, device="cuda", dtype=DT[dtype])
+    K, V = kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)
+    kept = np.stack([np.sort(rng.permutation(Hq)[:k_h]) for _ in range(B)]).astype(np.int32)
+    ids = masks = None
+    if run:
+        ids, masks = (np.arange(N) // run % 5).astype(np.int32), rng.integers(1, 32, B).astype(np.int32)
+    args = _cuda(kept, ids, masks)
+    sweep = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    out = []
+    for i in range(5):
+        sweep.fill_(i)
+        out.append(sn.cross_attend_fwd(Q, K, V, *args))
+    assert sn.last_status() == 0
+    assert all(torch.equal(o, out[0]) for o in out)
+    ok = ref.present(B, N, None, ids, masks)
+    for b in sorted({0, 3, 5, B // 2, B - 1} & set(range(B))):
+        q, o, here = Q[b].double().cpu().numpy(), out[0][b].double().cpu().numpy(), torch.from_numpy(ok[b]).cuda()
+        for j in range(0, k_h, 3):
+            h = int(kept[b, j])
+            k, v = (x[b, h * Hk // Hq][here].double().cpu().numpy() for x in (K, V))
+            want, tol = ref.attention(q[h], k, v, np.ones((Tq, len(k)), bool), DT[dtype], 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11)
+            ref.check(o[j], want, tol, "sample %d head %d" % (b, h))
+    del kv, K, V, sweep
+    torch.cuda.empty_cache()
