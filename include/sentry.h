@@ -17,7 +17,11 @@
  *   - All calls enqueue work on the CUDA stream passed as `stream`
  *     (a cudaStream_t cast to void*, NULL = default stream) and return without
  *     synchronising.  Calls that share a context and its workspace must be
- *     ordered on one stream (or otherwise not overlap).
+ *     ordered on one stream (or otherwise not overlap); a graph's replay counts
+ *     as the calls that were captured.  Calls that overlap all the same spoil
+ *     each other's results, and those of sentry_cross_attend_fwd and
+ *     sentry_cache_attend_fwd can leave the context's counters wrong for later
+ *     ones: such a context has to be replaced.
  *   - Return value: 0 = SENTRY_OK, negative = error found on the host BEFORE any
  *     launch (nothing was enqueued).  Conditions only the device can see (a
  *     sample with an empty modality mask, a bounded wait that ran out) are
@@ -588,7 +592,8 @@ SENTRY_API int sentry_cache_append(sentry_ctx* ctx, const sentry_kv_cache* cache
  * is fp16; all sums are fp32.  As for cross attention, with the products of a weight and its page's value scale in the place of the
  * weights: what is small beside the largest of them loses digits.  Value scales of the pages that a sample sees may differ by 2^64; values of
  * pages smaller yet lose digits.
- * e4m3 codes 0x7f and 0xff (NaN; sentry_cache_append writes none) give NaN.  Workspace: sentry_cache_workspace_bytes.
+ * e4m3 codes 0x7f and 0xff (NaN; sentry_cache_append writes none) among a sample's tokens give NaN, in V to rows that do not see
+ * them too (but for F32).  Workspace: sentry_cache_workspace_bytes.
  */
 typedef struct sentry_cache_attend_desc {
     int B, Tq, Hq, k_h, dtype, causal;
