@@ -10,12 +10,11 @@
 constexpr int kAppThreads = 256;
 constexpr int kHold = 8;          // pieces that a lane holds in registers
 
-// log2 of the team's warps.  A power of two of them, so that teams divide the block and masks give a lane's place: the most with which a
-// full page's lanes (min(page, T) rows of 2^row_shift pieces) have kHold pieces each, so that few have more than those to read twice.
-APPEND_FN int append_team_shift(int page, int T, int row_shift) {
-    const int wide = ((page < T ? page : T) << row_shift) / (32 * kHold);
-    return wide >= 8 ? 3 : wide >= 4 ? 2 : wide >= 2 ? 1 : 0;
+// Warps of a team.  A power of two, so that teams divide the block and masks give a lane's place: the most with which a full page's
+// lanes (min(page, T) rows of 2^row_shift pieces) have kHold pieces each, so that few have more than those to read twice.
+APPEND_FN int append_team(int page, int T, int row_shift) {
+    const int wide = ((page < T ? page : T) << row_shift) / (32 * kHold), most = wide < 1 ? 1 : wide > 8 ? 8 : wide;
+    return most & 8 ? 8 : most & 4 ? 4 : most & 2 ? 2 : 1;
 }
-// A lane's place in its team, and the team's among the block's: it takes pieces `place`, `place + lanes`, ...
-APPEND_FN int append_place(int warp, int lane, int team_shift) { return ((warp & ((1 << team_shift) - 1)) << 5) + lane; }
-APPEND_FN int append_lanes(int team_shift) { return 32 << team_shift; }
+// A lane's place in its team: it takes pieces `place`, `place + 32 team`, ...
+APPEND_FN int append_place(int warp, int lane, int team) { return ((warp & (team - 1)) << 5) + lane; }

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kAppThreads, 3) cache_append_kernel(const Appe
     __syncthreads();
     // (K or V, head) of a page: a team of warps
     const int shift = 31 - __clz(d / N), per_row = 1 << shift;       // pieces of a row
-    const int team_shift = append_team_shift(page, T_, shift), team = 1 << team_shift, lanes = append_lanes(team_shift), me = append_place(warp, lane, team_shift);
+    const int team = append_team(page, T_, shift), team_shift = 31 - __clz(team), lanes = 32 << team_shift, me = append_place(warp, lane, team);
     const int units = pages * 2 * Hk, at_a_time = (kAppThreads / 32) >> team_shift;
     for (int u0 = 0; u0 < units; u0 += at_a_time) {                  // (the same number of rounds for every warp)
         const int u = u0 + (warp >> team_shift), pi = u / (2 * Hk), unit = u - pi * 2 * Hk;

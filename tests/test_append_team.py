@@ -10,14 +10,14 @@ import pytest
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2604_08971_b200", "csrc")
 SOURCE = r"""
 #include "append_team.cuh"
-extern "C" int team_shift(int page, int T, int row_shift) { return append_team_shift(page, T, row_shift); }
+extern "C" int team(int page, int T, int row_shift) { return append_team(page, T, row_shift); }
 extern "C" int warps() { return kAppThreads / 32; }
 // how often each piece of each of the block's teams is taken, as cache_append_kernel walks them
-extern "C" void walk(int team_shift, int pieces, int* taken) {
+extern "C" void walk(int team, int pieces, int* taken) {
     for (int warp = 0; warp < kAppThreads / 32; ++warp)
         for (int lane = 0; lane < 32; ++lane) {
-            const int me = append_place(warp, lane, team_shift), lanes = append_lanes(team_shift);
-            int* mine = taken + (warp >> team_shift) * pieces;
+            const int me = append_place(warp, lane, team), lanes = 32 * team;
+            int* mine = taken + warp / team * pieces;
             for (int i = 0; i < kHold; ++i)
                 if (i * lanes + me < pieces) ++mine[i * lanes + me];
             for (int p = kHold * lanes + me; p < pieces; p += lanes) ++mine[p];
@@ -40,10 +40,10 @@ def host(tmp_path_factory):
 def test_every_piece_once(host, page, d, values):
     row_shift = (d // values).bit_length() - 1
     for T in list(range(1, page + 1)) + [page + 1, 10 * page + 3]:
-        team_shift = host.team_shift(page, T, row_shift)
-        assert 1 << team_shift <= host.warps()
-        teams = host.warps() >> team_shift
+        team = host.team(page, T, row_shift)
+        assert host.warps() % team == 0 and team & team - 1 == 0
+        teams = host.warps() // team
         for n in {1, (T + 1) // 2, min(page, T)}:          # tokens that fall into the page
             taken = np.zeros((teams, n << row_shift), np.int32)
-            host.walk(team_shift, n << row_shift, taken.ctypes.data_as(ctypes.c_void_p))
+            host.walk(team, n << row_shift, taken.ctypes.data_as(ctypes.c_void_p))
             assert (taken == 1).all(), (T, n)
