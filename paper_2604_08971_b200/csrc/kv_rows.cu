@@ -15,7 +15,8 @@
 // (Value scales that multiplied the weights, without the weights' 2^11, cost 0.6 us less here and lost small weights beside a large one.)
 // One token of 32 samples of up to 4096 e4m3 tokens (16 heads on 4, d 128, 87 MB): 25 us, 3.5 TB/s over all; a block's first keys arrive 3.5 us
 // after its start (lengths, page, keys: three loads that depend on one another), between that and the last tile the loads run at 5 to 5.7 TB/s,
-// and the parts meet in 3.  i8 of d 64 (2 x 131072 tokens, 67 MB): 29 us, where issue is as long as the bytes (640 instructions a warp for 32 keys).
+// and the parts meet in 3.  i8 of d 64 (2 x 131072 tokens, 67 MB): 29 us, issue slots 48 % and memory 36 % busy: some 640 instructions a warp for 32 keys, which wait
+// for one another at 16 working warps an SM.
 // Every wait is bounded; on expiry the block raises SENTRY_STATUS_BIT_TIMEOUT and unwinds.
 #include "kv_attend.cuh"
 #include "kv_maps.cuh"
