@@ -277,10 +277,11 @@ int launch_typed(sentry_ctx* ctx, const AttendArgs& a, cudaStream_t st) {
     const sentry_attend_desc& d = a.d;
     const int BH = d.B * d.k_h;
     const size_t valid_bytes = (((size_t)d.T * 2 + 15) / 16) * 16;
+    constexpr size_t kFree = 40 * 1024;              // of the 48 KB that need no permission, beside the static arrays
     if (!a.selection_given) {
         {
             auto kern = attend_score_kernel<T, D>;
-            if (valid_bytes > 48 * 1024)
+            if (valid_bytes > kFree)
                 SENTRY_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                      (int)valid_bytes));
             dim3 grid(BH, (d.T + kScoreThreads - 1) / kScoreThreads);   // (sample, head) on x: no 65535 limit
@@ -292,7 +293,7 @@ int launch_typed(sentry_ctx* ctx, const AttendArgs& a, cudaStream_t st) {
         SENTRY_CUDA_TRY(cudaGetLastError());
         {
             const size_t smem = valid_bytes + (size_t)d.T * 4;
-            if (smem > 48 * 1024)
+            if (smem > kFree)
                 SENTRY_CUDA_TRY(cudaFuncSetAttribute(attend_select_kernel,
                                                      cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                      (int)smem));
@@ -305,7 +306,7 @@ int launch_typed(sentry_ctx* ctx, const AttendArgs& a, cudaStream_t st) {
     {
         auto kern = attend_core_kernel<T, D>;
         const size_t smem = valid_bytes + (size_t)d.T;
-        if (smem > 48 * 1024)
+        if (smem > kFree)
             SENTRY_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)smem));
         LaunchScope ls(ctx, KS_ATT_CORE, st);

@@ -242,6 +242,11 @@ __global__ void gate_expand_kernel(const int32_t* __restrict__ rows,
 
 }  // namespace
 
+// (its static arrays count against the 48 KB that need no permission)
+static cudaError_t allow_gate_rows(size_t smem) {
+    return smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(gate_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
 int launch_gate_select(sentry_ctx* ctx, const float* scores, int S, int n_units,
                        const uint32_t* masks, int n_masks, int k, int32_t* kept,
                        uint32_t* kv_groups, int heads_per_group, int32_t* ws_rows,
@@ -252,9 +257,7 @@ int launch_gate_select(sentry_ctx* ctx, const float* scores, int S, int n_units,
         return launch_gate_reg(S, &g, 1, ctx->d_status, ctx->sm_count, st);
     }
     const size_t smem = (size_t)n_units * sizeof(uint32_t);
-    if (smem > 48 * 1024)
-        SENTRY_CUDA_TRY(cudaFuncSetAttribute(gate_rows_kernel,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    SENTRY_CUDA_TRY(allow_gate_rows(smem));
     const size_t total = (size_t)n_masks * k;
     {
         LaunchScope ls(ctx, KS_GATE_ROWS, st);
@@ -383,6 +386,7 @@ extern "C" int sentry_gate_select_static(int device, const float* scores, int S,
     }
     // The array keeps whatever the previous call left.  rows/groups are rewritten in full for
     // all S score rows before the fan-out reads them; only the status word must start at zero.
+    SENTRY_CUDA_TRY(allow_gate_rows((size_t)n_units * sizeof(uint32_t)));
     SENTRY_CUDA_TRY(cudaMemsetAsync(own_status, 0, sizeof(unsigned int), st));
     gate_rows_kernel<<<S, kGateMaxThreads, (size_t)n_units * sizeof(uint32_t), st>>>(
         scores, n_units, k, rows, kv_groups ? groups : nullptr, heads_per_group > 0 ? heads_per_group : 1);
