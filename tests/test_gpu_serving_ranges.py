@@ -268,3 +268,35 @@ def test_cross_attend_keys_beyond_the_l2(sn, case, dtype):
             ref.check(o[j], want, tol, "sample %d head %d" % (b, h))
     del kv, K, V, sweep
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("B,Tq,N,page", [FEW + (2100, 32), MANY + (2100, 32), (2, 3, 9001, 16), (3, 700, 5003, 64), FEW + (400, 16)])
+@pytest.mark.parametrize("large", [0, 1, 5])
+def test_value_scales_far_apart(sn, dtype, fmt, B, Tq, N, page, large):
+    """Every seventh page has values 2^60 times the others' and no weight to speak of: what the others hold is the result."""
+    d = 64
+    if dtype == "f32":
+        B = min(B, 3)
+    rng = np.random.default_rng(N)
+    cols, top = -(-N // page), 127 if fmt == "i8" else 448
+    q = np.where(np.arange(d) % 2, 1.0, -1.0)
+    far = np.arange(cols) % 7 == large
+    code = (lambda x: np.rint(x).astype(np.int8)) if fmt == "i8" else ref.to_e4m3
+    k = rng.uniform(-1, 1, (cols, page, 1)) * q * top
+    k[far] = -top * q
+    ks = np.full((cols, 1), 1.0 / (8 * top), np.float32)
+    ks[far] = 300.0 / (8 * top)                                # scores of -300
+    vs = (2.0 ** rng.uniform(-33, -30, (cols, 1))).astype(np.float32)
+    vs[far] *= np.float32(2.0 ** 60)
+    kc, vc = code(k).reshape(cols, 1, page, d), code(rng.uniform(-1, 1, (cols, 1, page, d)) * top)
+    table = np.broadcast_to(np.arange(cols, dtype=np.int32), (B, cols)).copy()
+    Q = torch.from_numpy(q).to(DT[dtype]).expand(B, 1, Tq, d).contiguous()
+    O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs, table, np.full(B, N, np.int32)))
+    kk, vv = ((ref.values(c, fmt) * s[..., None, None].astype(np.float64)).reshape(-1, d)[:N] for c, s in ((kc, ks), (vc, vs)))
+    if dtype == "f16":                                        # (its results are below half's range: in its smallest steps)
+        vv = vv * 2.0 ** 22
+        O = sn.cache_attend_fwd(Q.cuda(), *_cuda(kc, vc, ks, vs * np.float32(2.0 ** 22), table, np.full(B, N, np.int32)))
+    assert sn.last_status() == 0
+    _check_alike(O, q, kk, vv, DT[dtype], 2.0 ** -11 if dtype != "f32" else 0.0)
